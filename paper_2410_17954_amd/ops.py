@@ -83,6 +83,9 @@ def load_library(path=None):
         "moe_plec_layer": (I32, [P, I32, P, P, P, P, P, P]),
         "moe_plec_advance": (I32, [P, I32, P, P]),
         "moe_load_experts": (I32, [P, P, P, I32, P, P, P, I32, I64, I64, I32, P, P, I32, P]),
+        "moe_beam_select_workspace": (SZ, [I64, I32, I64, I32]),
+        "moe_beam_select": (I32, [P, I32, I64, I32, I64, P, P, I64, I32, P, P, P, P, P, SZ, P]),
+        "moe_beam_reorder": (I32, [P, I32, I64, I64, I32, I64, I64, P, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -103,6 +106,11 @@ def exported_symbols():
             "moe_probe_mfma_bf16", "moe_probe_read", "moe_probe_copy", "moe_plan_slots", "moe_plec_order",
             "moe_plec_run", "moe_lru_run", "moe_load_experts", "moe_plec_state_bytes",
             "moe_plec_begin", "moe_plec_layer", "moe_plec_advance"]
+
+
+def exported_decode_symbols():
+    """The entry points of include/moeflow_decode.h."""
+    return ["moe_beam_select_workspace", "moe_beam_select", "moe_beam_reorder"]
 
 
 def _check(name, status):
@@ -695,3 +703,102 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
                               _ptr(cd), S, H, F, _dtype_code(cg), ep, sp, int(e.shape[0]),
                               _stream(stream))
     _check("moe_load_experts", st)
+
+
+# ----------------------------------------------------------------- decode step
+def _one_device(*ts):
+    """Every given tensor contiguous, on one GPU: a context that makes it the
+    current device (its stream is then the one the call goes to)."""
+    _dev(*ts)
+    devs = {t.device for t in ts if t is not None}
+    if len(devs) != 1:
+        raise ValueError("every tensor must be on the same GPU")
+    return _torch().cuda.device(devs.pop())
+
+
+def _want(name, t, shape, dtype):
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+
+
+def beam_select_workspace(B, K, V, n_out):
+    return load_library().moe_beam_select_workspace(B, K, V, n_out)
+
+
+def beam_select(logits, scores, n_out=None, finished=None, eos=None, parent=None, token=None,
+                out_scores=None, out_finished=None, workspace=None, stream=None):
+    """moe_beam_select: the n_out (default K) best continuations of each request.
+    logits [B, K, V] bfloat16 or float32, scores float32 [B, K], finished int32
+    [B, K] or None. Returns (parent int32 [B, n_out], rows b*K + beam; token
+    int32; score float32; finished int32, or None without an eos)."""
+    torch = _torch()
+    lib = load_library()
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, K, V]")
+    B, K, V = logits.shape
+    n_out = K if n_out is None else int(n_out)
+    dt = _dtype_code(logits)
+    if finished is not None and eos is None:
+        raise ValueError("finished beams need an eos token")
+    if out_finished is not None and eos is None:
+        raise ValueError("out_finished needs an eos token")
+    _want("scores", scores, (B, K), torch.float32)
+    _want("finished", finished, (B, K), torch.int32)
+    for name, t in (("parent", parent), ("token", token), ("out_finished", out_finished)):
+        _want(name, t, (B, n_out), torch.int32)
+    _want("out_scores", out_scores, (B, n_out), torch.float32)
+    with _one_device(logits, scores, finished, parent, token, out_scores, out_finished,
+                     workspace):
+        new = lambda t, dtype: torch.empty((B, n_out), dtype=dtype, device=logits.device) \
+            if t is None else t
+        parent, token = new(parent, torch.int32), new(token, torch.int32)
+        out_scores = new(out_scores, torch.float32)
+        if eos is not None:
+            out_finished = new(out_finished, torch.int32)
+        ws, nbytes = _workspace(lib.moe_beam_select_workspace(B, K, V, n_out), logits.device,
+                                workspace)
+        st = lib.moe_beam_select(_ptr(logits), dt, B, K, V, _ptr(scores), _ptr(finished),
+                                 -1 if eos is None else int(eos), n_out, _ptr(parent), _ptr(token),
+                                 _ptr(out_scores), _ptr(out_finished), _ptr(ws), nbytes,
+                                 _stream(stream))
+    _check("moe_beam_select", st)
+    return parent, token, out_scores, out_finished
+
+
+def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None):
+    """moe_beam_reorder: caches, a list of up to 16 tensors [L, B*K, S, ...] of
+    any dtype (one trailing size in bytes), updated in place; parent int32
+    [B, K] as beam_select writes it (n_out = K); lens int32 [B*K] or None (every
+    position). Returns (new_lens int32 [B*K], err int32 [1])."""
+    torch = _torch()
+    lib = load_library()
+    if not caches or len(caches) > 16:
+        raise ValueError("1 to 16 caches")
+    if parent.dim() != 2 or parent.dtype != torch.int32:
+        raise ValueError("parent must be int32 [B, K]")
+    B, K = parent.shape
+    R = B * K
+    L, _, S = caches[0].shape[:3]
+    unit = caches[0].element_size()
+    for d in caches[0].shape[3:]:
+        unit *= d
+    for c in caches:
+        n = c.element_size()
+        for d in c.shape[3:]:
+            n *= d
+        if c.dim() < 3 or tuple(c.shape[:3]) != (L, R, S) or n != unit:
+            raise ValueError("caches must be [L, B*K, S, ...] with equal bytes a position")
+    _want("lens", lens, (R,), torch.int32)
+    _want("new_lens", new_lens, (R,), torch.int32)
+    _want("err", err, (1,), torch.int32)
+    with _one_device(*caches, parent, lens, new_lens, err):
+        dev = parent.device
+        if new_lens is None:
+            new_lens = torch.empty(R, dtype=torch.int32, device=dev)
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=dev)
+        ptrs = (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches])
+        st = lib.moe_beam_reorder(ptrs, len(caches), L, B, K, S, unit, _ptr(parent), _ptr(lens),
+                                  _ptr(new_lens), _ptr(err), _stream(stream))
+    _check("moe_beam_reorder", st)
+    return new_lens, err

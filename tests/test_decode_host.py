@@ -1,0 +1,116 @@
+"""CPU checks of the decode-step entry points (include/moeflow_decode.h): the
+declared symbols are exported, invalid arguments are rejected on the host before
+a device is touched, and the oracle's pins."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+
+import oracle
+from paper_2410_17954_amd import ops
+from paper_2410_17954_amd.build import library_path
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "moeflow_decode.h")
+FAKE = ctypes.c_void_p(0x1000)      # never dereferenced: validation fails first
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(library_path()):
+        from paper_2410_17954_amd import build
+        build.build(verbose=False)
+    return ops.load_library()
+
+
+def test_every_declared_symbol_is_exported(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = re.findall(r"^\s*(?:const\s+)?\w+\*?\s+\*?(moe_\w+)\s*\(", text, re.M)
+    assert sorted(names) == sorted(ops.exported_decode_symbols())
+    for n in names:
+        assert hasattr(lib, n)
+
+
+def test_beam_select_rejects_bad_arguments(lib):
+    S = None
+
+    def call(logits=FAKE, dt=1, B=2, K=4, V=100, scores=FAKE, fin=S, eos=0, n=4, parent=FAKE,
+             token=FAKE, best=FAKE, flags=S, ws=FAKE, nbytes=BIG):
+        return lib.moe_beam_select(logits, dt, B, K, V, scores, fin, eos, n, parent, token, best,
+                                   flags, ws, nbytes, S)
+
+    for bad in (dict(logits=S), dict(scores=S), dict(parent=S), dict(token=S), dict(best=S),
+                dict(dt=2), dict(B=0), dict(K=0), dict(V=0), dict(n=0), dict(fin=FAKE, eos=100),
+                dict(flags=FAKE, eos=-1), dict(logits=ctypes.c_void_p(0x1001)),
+                dict(dt=0, logits=ctypes.c_void_p(0x1002))):
+        assert call(**bad) == ops.MOE_ERR_ARG, bad
+    for bad in (dict(K=33), dict(n=65), dict(V=(1 << 23) + 1), dict(B=1 << 31)):
+        assert call(**bad) == ops.MOE_ERR_UNSUPPORTED, bad
+    need = lib.moe_beam_select_workspace(2, 4, 100, 4)
+    assert need > 0 and need % 256 == 0
+    for bad in (dict(ws=S), dict(nbytes=need - 1), dict(ws=ctypes.c_void_p(0x1010))):
+        assert call(**bad) == ops.MOE_ERR_WORKSPACE, bad
+    for bad in ((0, 4, 100, 4), (2, 33, 100, 4), (2, 4, 0, 4), (2, 4, 100, 65)):
+        assert lib.moe_beam_select_workspace(*bad) == 0
+
+
+def test_beam_reorder_rejects_bad_arguments(lib):
+    S = None
+    two = (ctypes.c_void_p * 2)(0x1000, 0x2000)
+
+    def call(caches=two, n=2, L=2, B=2, K=4, s=8, unit=64, parent=FAKE, lens=FAKE,
+             new=ctypes.c_void_p(0x3000), err=FAKE):
+        return lib.moe_beam_reorder(caches, n, L, B, K, s, unit, parent, lens, new, err, S)
+
+    for bad in (dict(caches=S), dict(n=0), dict(n=17), dict(L=0), dict(B=0), dict(K=0),
+                dict(s=-1), dict(unit=0), dict(parent=S), dict(err=S), dict(new=FAKE),
+                dict(caches=(ctypes.c_void_p * 2)(0x1000, None)),
+                dict(caches=(ctypes.c_void_p * 2)(0x1000, 0x1000))):
+        assert call(**bad) == ops.MOE_ERR_ARG, bad
+    for bad in (dict(K=33), dict(unit=1 << 31), dict(s=1 << 25, unit=64), dict(B=1 << 30),
+                dict(L=1 << 50)):
+        assert call(**bad) == ops.MOE_ERR_UNSUPPORTED, bad
+
+
+# ------------------------------------------------------------------ oracle pins
+def test_oracle_select_is_the_sort_of_all_candidates():
+    g = np.random.default_rng(1)
+    B, K, V, n = 3, 4, 11, 7
+    z, s = g.normal(size=(B, K, V)), g.normal(size=(B, K))
+    parent, token, score, _ = oracle.beam_select(z, s, n)
+    p = np.exp(z) / np.exp(z).sum(-1, keepdims=True)
+    c = np.log(p) + s[..., None]
+    for b in range(B):
+        order = np.argsort(-c[b].ravel(), kind="stable")[:n]
+        assert np.array_equal(parent[b], b * K + order // V)
+        assert np.array_equal(token[b], order % V)
+        assert np.allclose(score[b], c[b].ravel()[order], rtol=0, atol=1e-12)
+
+
+def test_oracle_select_special_rows():
+    z = np.zeros((1, 3, 4))
+    s = np.array([[0.0, -1.0, -np.inf]])
+    parent, token, score, done = oracle.beam_select(z, s, 6, finished=np.array([[0, 1, 0]]), eos=3)
+    # beam 0: four equal tokens of probability 1/4; beam 1: only the end token, at its score
+    assert parent[0].tolist() == [1, 0, 0, 0, 0, -1]
+    assert token[0].tolist() == [3, 0, 1, 2, 3, -1]
+    assert np.allclose(score[0, :5], [-1.0] + [np.log(0.25)] * 4) and score[0, 5] == -np.inf
+    assert done[0].tolist() == [1, 0, 0, 0, 1, 0]
+    z[0, 0, 2] = np.nan                                 # no candidate of a row with a NaN
+    assert oracle.beam_select(z, s, 2)[0][0].tolist() == [1, 1]
+
+
+def test_oracle_reorder_moves_all_rows_at_once():
+    cache = np.arange(2 * 4 * 3).reshape(2, 4, 3)
+    out, lens, bad = oracle.beam_reorder(cache, [1, 0, 2, 2], 2, lens=[1, 3, 2, 0])
+    assert not bad and lens.tolist() == [3, 1, 2, 2]
+    assert np.array_equal(out[:, 0], cache[:, 1])       # three positions
+    assert np.array_equal(out[:, 1, :1], cache[:, 0, :1])
+    assert np.array_equal(out[:, 1, 1:], cache[:, 1, 1:])
+    assert np.array_equal(out[:, 3, :2], cache[:, 2, :2])
+    out, lens, bad = oracle.beam_reorder(cache, [2, -1, 3, 9], 2)
+    assert bad and np.array_equal(out[:, [0, 1, 3]], cache[:, [0, 1, 3]])
+    assert np.array_equal(out[:, 2], cache[:, 3])
