@@ -25,6 +25,49 @@ extern "C" {
 #endif
 
 /* ------------------------------------------------------------------------
+ * moe_layer_decode -- a whole MoE layer (Sec. 2.1) for the T <= 64 tokens of a
+ * decode step: what moe_route, moe_permute, moe_expert_ffn and moe_combine
+ * compute together, without the maps and row copies between them:
+ *
+ *   z[t, e]   = x_t . w_router[e] (+ bias), in float64
+ *   idx[t, :] = the k largest z[t, :], descending; equal ones go to the lower
+ *               expert; a NaN is never chosen (fewer than k numbers: idx -1,
+ *               gate 0)
+ *   w[t, j]   = softmax(z[t, :])[idx[t, j]], with renormalize divided by their
+ *               sum over j
+ *   y[t]      = (accumulate: y[t] +) sum_{j: slot(idx) in 0..S-1} w[t, j] E(x_t)
+ *               + Shared(x_t)
+ *   E(x)      = w_down . a,  a = silu(w_gate . x) * (w_up . x)
+ * float32 accumulation; w[t, j] * a is rounded to dtype once, as the operand of
+ * the down projection, and y once.
+ *
+ * x [T, H], w_router [E, H], bias as for moe_route (bias_mode 0: NULL, 1: [E],
+ * 2: [T, E]); w_gate, w_up [S, F, H], w_down [S, H, F]: the expert slots;
+ * slot_of_expert [E] int32 (outside 0..S-1: not resident) or NULL (expert e in
+ * slot e, S >= E)
+ * shared_gate, shared_up [Fs, H], shared_down [H, Fs]: the always-on experts,
+ *   concatenated along Fs; NULL with Fs == 0
+ * y          [T, H] dtype output, may be x; no other overlap is allowed
+ * topk_idx, topk_w  [T, k] outputs
+ * incomplete [T] int32 output or NULL: 1 when some choice is not resident
+ * workspace  moe_layer_decode_workspace bytes, 256-byte aligned
+ * Results do not depend on scheduling: sums run in a fixed order.
+ * Limits: 1 <= T <= 64, 1 <= k <= min(E, 32), E <= 256; H, F, Fs multiples of 8
+ *   (bf16) or 4 (float32), at most 2^22, 2^24, 2^24; tensors of dtype on 16 bytes;
+ *   (T*k*F + T*Fs) values below 2 GiB; else MOE_ERR_UNSUPPORTED (the four calls
+ *   take such batches). Errors: MOE_ERR_ARG, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
+ * ---------------------------------------------------------------------- */
+size_t moe_layer_decode_workspace(int64_t T, int64_t H, int64_t F, int32_t E, int32_t k,
+                                  int64_t Fs, int32_t dtype);
+int moe_layer_decode(const void* x, int32_t dtype, int64_t T, int64_t H, const void* w_router,
+                     int32_t E, int32_t k, const float* bias, int32_t bias_mode,
+                     int32_t renormalize, const void* w_gate, const void* w_up,
+                     const void* w_down, int32_t S, int64_t F, const int32_t* slot_of_expert,
+                     const void* shared_gate, const void* shared_up, const void* shared_down,
+                     int64_t Fs, int32_t accumulate, void* y, int32_t* topk_idx, float* topk_w,
+                     int32_t* incomplete, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * moe_beam_select -- the n_out best continuations of each of B requests over
  * its K beams and V tokens:
  *

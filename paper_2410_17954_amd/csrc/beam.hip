@@ -11,6 +11,7 @@
 // whatever the logits hold.
 #include "moeflow_decode.h"
 #include "common.h"
+#include "buffers.h"
 
 #include <algorithm>
 
@@ -352,7 +353,6 @@ struct ReCaches { char* base[kReMaxCaches]; };
 
 // 16, 8, 4 or 1 bytes of a raw buffer per lane; past its end nothing is read
 // (zeros) or written.
-typedef __amdgpu_buffer_rsrc_t rsrc_t;
 template <int ELT> struct Piece;
 template <> struct Piece<16> {
   using T = u32x4_t;

@@ -83,6 +83,9 @@ def load_library(path=None):
         "moe_plec_layer": (I32, [P, I32, P, P, P, P, P, P]),
         "moe_plec_advance": (I32, [P, I32, P, P]),
         "moe_load_experts": (I32, [P, P, P, I32, P, P, P, I32, I64, I64, I32, P, P, I32, P]),
+        "moe_layer_decode_workspace": (SZ, [I64, I64, I64, I32, I32, I64, I32]),
+        "moe_layer_decode": (I32, [P, I32, I64, I64, P, I32, I32, P, I32, I32, P, P, P, I32, I64,
+                                   P, P, P, P, I64, I32, P, P, P, P, P, SZ, P]),
         "moe_beam_select_workspace": (SZ, [I64, I32, I64, I32]),
         "moe_beam_select": (I32, [P, I32, I64, I32, I64, P, P, I64, I32, P, P, P, P, P, SZ, P]),
         "moe_beam_reorder": (I32, [P, I32, I64, I64, I32, I64, I64, P, P, P, P, P]),
@@ -110,7 +113,8 @@ def exported_symbols():
 
 def exported_decode_symbols():
     """The entry points of include/moeflow_decode.h."""
-    return ["moe_beam_select_workspace", "moe_beam_select", "moe_beam_reorder"]
+    return ["moe_layer_decode_workspace", "moe_layer_decode", "moe_beam_select_workspace",
+            "moe_beam_select", "moe_beam_reorder"]
 
 
 def _check(name, status):
@@ -719,6 +723,70 @@ def _one_device(*ts):
 def _want(name, t, shape, dtype):
     if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+
+
+def layer_decode_workspace(T, H, F, E, k, Fs=0, dtype_code=MOE_BF16):
+    return load_library().moe_layer_decode_workspace(T, H, F, E, k, Fs, dtype_code)
+
+
+def layer_decode(x, w_router, w_gate, w_up, w_down, k, bias=None, renormalize=True,
+                 slot_of_expert=None, shared=None, y=None, accumulate=False, topk_idx=None,
+                 topk_w=None, incomplete=None, want_incomplete=True, workspace=None, stream=None):
+    """moe_layer_decode: a whole MoE layer for x [T, H], T <= 64. w_router [E, H],
+    w_gate/w_up [S, F, H], w_down [S, H, F]; shared = (gate [Fs, H], up [Fs, H],
+    down [H, Fs]) or None; y may be x, and must be given with accumulate. Returns
+    (y [T, H], topk_idx int32 [T, k], topk_w float32 [T, k], incomplete int32 [T]
+    or None)."""
+    torch = _torch()
+    lib = load_library()
+    if x.dim() != 2 or w_router.dim() != 2 or w_gate.dim() != 3:
+        raise ValueError("x [T, H], w_router [E, H], w_gate [S, F, H]")
+    T, H = x.shape
+    E = w_router.shape[0]
+    S, F = w_gate.shape[:2]
+    k = int(k)
+    dt = _dtype_code(x)
+    _want("w_router", w_router, (E, H), x.dtype)
+    for name, t, shape in (("w_gate", w_gate, (S, F, H)), ("w_up", w_up, (S, F, H)),
+                           ("w_down", w_down, (S, H, F)), ("y", y, (T, H))):
+        _want(name, t, shape, x.dtype)
+    bias_mode = 0
+    if bias is not None:
+        bias_mode = 1 if bias.dim() == 1 else 2
+        _want("bias", bias, (E,) if bias_mode == 1 else (T, E), torch.float32)
+    Fs, sg, su, sd = 0, None, None, None
+    if shared is not None:
+        sg, su, sd = shared
+        Fs = sg.shape[0]
+        for name, t, shape in (("shared gate", sg, (Fs, H)), ("shared up", su, (Fs, H)),
+                               ("shared down", sd, (H, Fs))):
+            _want(name, t, shape, x.dtype)
+    _want("slot_of_expert", slot_of_expert, (E,), torch.int32)
+    _want("topk_idx", topk_idx, (T, k), torch.int32)
+    _want("topk_w", topk_w, (T, k), torch.float32)
+    _want("incomplete", incomplete, (T,), torch.int32)
+    if accumulate and y is None:
+        raise ValueError("accumulate needs an existing y")
+    with _one_device(x, w_router, w_gate, w_up, w_down, bias, slot_of_expert, sg, su, sd, y,
+                     topk_idx, topk_w, incomplete, workspace):
+        dev = x.device
+        if y is None:
+            y = torch.empty_like(x)
+        if topk_idx is None:
+            topk_idx = torch.empty((T, k), dtype=torch.int32, device=dev)
+        if topk_w is None:
+            topk_w = torch.empty((T, k), dtype=torch.float32, device=dev)
+        if incomplete is None and want_incomplete:
+            incomplete = torch.empty(T, dtype=torch.int32, device=dev)
+        ws, nbytes = _workspace(lib.moe_layer_decode_workspace(T, H, F, E, k, Fs, dt), dev,
+                                workspace)
+        st = lib.moe_layer_decode(_ptr(x), dt, T, H, _ptr(w_router), E, k, _ptr(bias), bias_mode,
+                                  1 if renormalize else 0, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                                  S, F, _ptr(slot_of_expert), _ptr(sg), _ptr(su), _ptr(sd), Fs,
+                                  1 if accumulate else 0, _ptr(y), _ptr(topk_idx), _ptr(topk_w),
+                                  _ptr(incomplete), _ptr(ws), nbytes, _stream(stream))
+    _check("moe_layer_decode", st)
+    return y, topk_idx, topk_w, incomplete
 
 
 def beam_select_workspace(B, K, V, n_out):

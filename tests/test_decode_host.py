@@ -75,6 +75,34 @@ def test_beam_reorder_rejects_bad_arguments(lib):
         assert call(**bad) == ops.MOE_ERR_UNSUPPORTED, bad
 
 
+def test_layer_decode_rejects_bad_arguments(lib):
+    S = None
+
+    def call(x=FAKE, dt=1, T=4, H=64, wr=FAKE, E=8, k=2, bias=S, mode=0, renorm=1, wg=FAKE,
+             wu=FAKE, wd=FAKE, s=8, F=128, slot=S, sg=S, su=S, sd=S, Fs=0, acc=0, y=FAKE, idx=FAKE,
+             w=FAKE, inc=S, ws=FAKE, nbytes=BIG):
+        return lib.moe_layer_decode(x, dt, T, H, wr, E, k, bias, mode, renorm, wg, wu, wd, s, F,
+                                    slot, sg, su, sd, Fs, acc, y, idx, w, inc, ws, nbytes, S)
+
+    for bad in (dict(x=S), dict(wr=S), dict(wg=S), dict(wu=S), dict(wd=S), dict(y=S), dict(idx=S),
+                dict(w=S), dict(dt=2), dict(T=0), dict(H=0), dict(F=0), dict(E=0), dict(E=257),
+                dict(k=0), dict(k=9), dict(s=7), dict(s=0, slot=FAKE), dict(bias=FAKE),
+                dict(mode=1), dict(mode=3, bias=FAKE), dict(renorm=2), dict(acc=2),
+                dict(Fs=64), dict(sg=FAKE), dict(Fs=64, sg=FAKE, su=FAKE), dict(Fs=-8)):
+        assert call(**bad) == ops.MOE_ERR_ARG, bad
+    odd = ctypes.c_void_p(0x1008)
+    for bad in (dict(T=65), dict(H=60), dict(F=124), dict(Fs=4, sg=FAKE, su=FAKE, sd=FAKE),
+                dict(dt=0, H=62), dict(E=64, k=33, s=64), dict(x=odd), dict(wd=odd), dict(y=odd),
+                dict(H=(1 << 22) + 8), dict(F=(1 << 24) + 8), dict(T=64, k=8, F=1 << 22)):
+        assert call(**bad) == ops.MOE_ERR_UNSUPPORTED, bad
+    need = lib.moe_layer_decode_workspace(4, 64, 128, 8, 2, 0, 1)
+    assert need >= 4 * 2 * 128 * 2 + 4 * 8 * 8
+    for bad in (dict(ws=S), dict(nbytes=need - 1), dict(ws=ctypes.c_void_p(0x1010))):
+        assert call(**bad) == ops.MOE_ERR_WORKSPACE, bad
+    assert lib.moe_layer_decode_workspace(65, 64, 128, 8, 2, 0, 1) == 0
+    assert lib.moe_layer_decode_workspace(4, 64, 128, 8, 9, 0, 1) == 0
+
+
 # ------------------------------------------------------------------ oracle pins
 def test_oracle_select_is_the_sort_of_all_candidates():
     g = np.random.default_rng(1)
