@@ -25,6 +25,45 @@ extern "C" {
 #endif
 
 /* ------------------------------------------------------------------------
+ * moe_prefix_attention -- softmax attention of R rows, one new token each.
+ * Group g's rows group_offsets[g] .. group_offsets[g+1]-1 share the keys and
+ * values of prefix g (a prompt whose beams they are, a prompt that a whole batch
+ * starts with); every row r goes on with its own suffix (the tokens since, the
+ * new one included):
+ *
+ *   s_i       = scale * q[r, h] . K_i over the keys of head h / (Hq / Hkv):
+ *               k_prefix[g, 0 .. prefix_len[g]), k_suffix[r, 0 .. suffix_len[r])
+ *   out[r, h] = sum_i softmax(s)_i V_i,  lse[r, h] = ln sum_i exp s_i
+ * A row without any key: out 0, lse -inf. Float32 scores, statistics and
+ * accumulation; bf16: the softmax numerators are rounded to bf16 for the second
+ * product, their sum is not. Results do not depend on scheduling.
+ *
+ * q, out         [R, Hq, D] dtype; lse [R, Hq] float32 or NULL
+ * group_offsets  [G+1] int32, non-decreasing (clipped to 0..R), or NULL: G equal
+ *                groups (R a multiple of G). Rows before the first and from the
+ *                last offset on belong to no group: out and lse keep what they
+ *                hold there
+ * k_prefix, v_prefix  [G, P, Hkv, D] dtype (may be NULL when P == 0)
+ * k_suffix, v_suffix  [R, S, Hkv, D] dtype (may be NULL when S == 0)
+ * prefix_len [G], suffix_len [R] int32 (clipped to 0..P, 0..S) or NULL (all).
+ *                What the caches hold from a length on is not used, be it NaN
+ * workspace      moe_prefix_attention_workspace bytes, 256-byte aligned (0 and
+ *                NULL when P == S == 0)
+ * Limits: R >= 1, 1 <= G <= R, Hq a multiple of Hkv, D a multiple of 8 up to
+ *   256, P, S < 2^31, Hkv * D * element size < 2^26, tensors of dtype on 16
+ *   bytes, scale finite. Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED,
+ *   MOE_ERR_WORKSPACE, MOE_ERR_HIP.
+ * ---------------------------------------------------------------------- */
+size_t moe_prefix_attention_workspace(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D,
+                                      int64_t P, int64_t S, int32_t dtype);
+int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, int32_t Hkv,
+                         int32_t D, const int32_t* group_offsets, int64_t G, const void* k_prefix,
+                         const void* v_prefix, int64_t P, const int32_t* prefix_len,
+                         const void* k_suffix, const void* v_suffix, int64_t S,
+                         const int32_t* suffix_len, float scale, void* out, float* lse,
+                         void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * moe_layer_decode -- a whole MoE layer (Sec. 2.1) for the T <= 64 tokens of a
  * decode step: what moe_route, moe_permute, moe_expert_ffn and moe_combine
  * compute together, without the maps and row copies between them:

@@ -28,6 +28,7 @@ Modules and the passages they follow:
                a residual stack of pre-normalised layers
   kv        -- KV-cache Merge and Reindex of Sec. 3.3.3
   rpp       -- forward pass of the routing path predictor of Sec. 3.2
+  attention -- attention over a shared prefix and own suffixes
   beam      -- selection over beams and vocabulary, states following their beams
 """
 from .gating import router_logits, topk_select, softmax, gate_weights, route
@@ -41,6 +42,7 @@ from .slots import plan_slots
 from .cache import plec_order, plec_run, lru_run
 from .layer import moe_layer, dense_ffn, moe_stack, round_bf16, rms_norm
 from .kv import kv_merge, kv_gather, kv_reindex
+from .attention import prefix_attention
 from .beam import beam_select, beam_reorder
 from . import rpp
 
@@ -52,5 +54,6 @@ __all__ = [
     "schedule_multi", "plan_slots",
     "plec_order", "plec_run", "lru_run",
     "moe_layer", "dense_ffn", "moe_stack", "round_bf16", "rms_norm",
-    "kv_merge", "kv_gather", "kv_reindex", "beam_select", "beam_reorder", "rpp",
+    "kv_merge", "kv_gather", "kv_reindex", "prefix_attention", "beam_select",
+    "beam_reorder", "rpp",
 ]

@@ -83,6 +83,9 @@ def load_library(path=None):
         "moe_plec_layer": (I32, [P, I32, P, P, P, P, P, P]),
         "moe_plec_advance": (I32, [P, I32, P, P]),
         "moe_load_experts": (I32, [P, P, P, I32, P, P, P, I32, I64, I64, I32, P, P, I32, P]),
+        "moe_prefix_attention_workspace": (SZ, [I64, I64, I32, I32, I32, I64, I64, I32]),
+        "moe_prefix_attention": (I32, [P, I32, I64, I32, I32, I32, P, I64, P, P, I64, P, P, P, I64,
+                                       P, ctypes.c_float, P, P, P, SZ, P]),
         "moe_layer_decode_workspace": (SZ, [I64, I64, I64, I32, I32, I64, I32]),
         "moe_layer_decode": (I32, [P, I32, I64, I64, P, I32, I32, P, I32, I32, P, P, P, I32, I64,
                                    P, P, P, P, I64, I32, P, P, P, P, P, SZ, P]),
@@ -113,7 +116,8 @@ def exported_symbols():
 
 def exported_decode_symbols():
     """The entry points of include/moeflow_decode.h."""
-    return ["moe_layer_decode_workspace", "moe_layer_decode", "moe_beam_select_workspace",
+    return ["moe_prefix_attention_workspace", "moe_prefix_attention",
+            "moe_layer_decode_workspace", "moe_layer_decode", "moe_beam_select_workspace",
             "moe_beam_select", "moe_beam_reorder"]
 
 
@@ -723,6 +727,62 @@ def _one_device(*ts):
 def _want(name, t, shape, dtype):
     if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+
+
+def prefix_attention_workspace(R, G, Hq, Hkv, D, P, S, dtype_code=MOE_BF16):
+    return load_library().moe_prefix_attention_workspace(R, G, Hq, Hkv, D, P, S, dtype_code)
+
+
+def prefix_attention(q, k_prefix=None, v_prefix=None, k_suffix=None, v_suffix=None,
+                     prefix_len=None, suffix_len=None, group_offsets=None, scale=None, out=None,
+                     lse=None, want_lse=True, workspace=None, stream=None):
+    """moe_prefix_attention. q [R, Hq, D]; k_prefix/v_prefix [G, P, Hkv, D] and
+    k_suffix/v_suffix [R, S, Hkv, D], either pair may be None; prefix_len int32
+    [G], suffix_len int32 [R]; group_offsets int32 [G+1] or None (G equal
+    groups); scale defaults to 1/sqrt(D). Returns (out [R, Hq, D], lse float32
+    [R, Hq] or None)."""
+    torch = _torch()
+    lib = load_library()
+    if q.dim() != 3:
+        raise ValueError("q must be [R, Hq, D]")
+    R, Hq, D = q.shape
+    dt = _dtype_code(q)
+    if (k_prefix is None) != (v_prefix is None) or (k_suffix is None) != (v_suffix is None):
+        raise ValueError("keys and values go together")
+    if k_prefix is None and k_suffix is None:
+        raise ValueError("a prefix or a suffix is needed")
+    for t in (k_prefix, k_suffix):
+        if t is not None and t.dim() != 4:
+            raise ValueError("caches must be [rows or groups, positions, Hkv, D]")
+    Hkv = (k_prefix if k_prefix is not None else k_suffix).shape[2]
+    G, P = (1, 0) if k_prefix is None else k_prefix.shape[:2]
+    if k_prefix is None and group_offsets is not None:
+        G = group_offsets.shape[0] - 1
+    S = 0 if k_suffix is None else k_suffix.shape[1]
+    for name, t in (("k_prefix", k_prefix), ("v_prefix", v_prefix)):
+        _want(name, t, (G, P, Hkv, D), q.dtype)
+    for name, t in (("k_suffix", k_suffix), ("v_suffix", v_suffix)):
+        _want(name, t, (R, S, Hkv, D), q.dtype)
+    _want("prefix_len", prefix_len, (G,), torch.int32)
+    _want("suffix_len", suffix_len, (R,), torch.int32)
+    _want("group_offsets", group_offsets, (G + 1,), torch.int32)
+    _want("out", out, (R, Hq, D), q.dtype)
+    _want("lse", lse, (R, Hq), torch.float32)
+    with _one_device(q, k_prefix, v_prefix, k_suffix, v_suffix, prefix_len, suffix_len,
+                     group_offsets, out, lse, workspace):
+        if out is None:                # rows of no group are left as they are
+            out = torch.empty_like(q) if group_offsets is None else torch.zeros_like(q)
+        if lse is None and want_lse:
+            lse = torch.full((R, Hq), -float("inf"), dtype=torch.float32, device=q.device)
+        ws, nbytes = _workspace(
+            lib.moe_prefix_attention_workspace(R, G, Hq, Hkv, D, P, S, dt), q.device, workspace)
+        st = lib.moe_prefix_attention(
+            _ptr(q), dt, R, Hq, Hkv, D, _ptr(group_offsets), G, _ptr(k_prefix), _ptr(v_prefix), P,
+            _ptr(prefix_len), _ptr(k_suffix), _ptr(v_suffix), S, _ptr(suffix_len),
+            float(D ** -0.5 if scale is None else scale), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
+            _stream(stream))
+    _check("moe_prefix_attention", st)
+    return out, lse
 
 
 def layer_decode_workspace(T, H, F, E, k, Fs=0, dtype_code=MOE_BF16):

@@ -103,6 +103,31 @@ def test_layer_decode_rejects_bad_arguments(lib):
     assert lib.moe_layer_decode_workspace(4, 64, 128, 8, 9, 0, 1) == 0
 
 
+def test_prefix_attention_rejects_bad_arguments(lib):
+    S = None
+
+    def call(q=FAKE, dt=1, R=4, Hq=8, Hkv=2, D=64, off=S, G=2, kp=FAKE, vp=FAKE, P=100, pl=S,
+             ks=FAKE, vs=FAKE, s=10, sl=S, scale=0.125, out=FAKE, lse=S, ws=FAKE, nbytes=BIG):
+        return lib.moe_prefix_attention(q, dt, R, Hq, Hkv, D, off, G, kp, vp, P, pl, ks, vs, s, sl,
+                                        scale, out, lse, ws, nbytes, S)
+
+    for bad in (dict(q=S), dict(out=S), dict(dt=3), dict(R=0), dict(G=0), dict(Hq=0), dict(Hkv=0),
+                dict(Hq=9), dict(D=0), dict(P=-1), dict(s=-1), dict(kp=S), dict(vp=S), dict(ks=S),
+                dict(vs=S), dict(G=3), dict(scale=float("nan")), dict(scale=float("inf"))):
+        assert call(**bad) == ops.MOE_ERR_ARG, bad
+    odd = ctypes.c_void_p(0x1008)
+    for bad in (dict(D=60), dict(D=264), dict(G=5, off=FAKE), dict(P=1 << 31), dict(s=1 << 31),
+                dict(q=odd), dict(kp=odd), dict(vs=odd), dict(out=odd),
+                dict(Hq=1 << 20, Hkv=1 << 20), dict(R=1 << 30, off=FAKE)):
+        assert call(**bad) == ops.MOE_ERR_UNSUPPORTED, bad
+    need = lib.moe_prefix_attention_workspace(4, 2, 8, 2, 64, 100, 10, 1)
+    assert need >= 2 * 4 * 8 * (64 * 4 + 8)
+    for bad in (dict(ws=S), dict(nbytes=need - 1), dict(ws=ctypes.c_void_p(0x1010))):
+        assert call(**bad) == ops.MOE_ERR_WORKSPACE, bad
+    assert lib.moe_prefix_attention_workspace(4, 2, 8, 2, 64, 0, 0, 1) == 0
+    assert lib.moe_prefix_attention_workspace(4, 5, 8, 2, 64, 100, 10, 1) == 0
+
+
 # ------------------------------------------------------------------ oracle pins
 def test_oracle_select_is_the_sort_of_all_candidates():
     g = np.random.default_rng(1)
@@ -142,3 +167,29 @@ def test_oracle_reorder_moves_all_rows_at_once():
     out, lens, bad = oracle.beam_reorder(cache, [2, -1, 3, 9], 2)
     assert bad and np.array_equal(out[:, [0, 1, 3]], cache[:, [0, 1, 3]])
     assert np.array_equal(out[:, 2], cache[:, 3])
+
+
+def test_oracle_attention_closed_forms():
+    g = np.random.default_rng(3)
+    R, Hq, Hkv, D, P, S = 3, 4, 2, 8, 5, 4
+    q = g.normal(size=(R, Hq, D))
+    kp, vp = g.normal(size=(2, P, Hkv, D)), g.normal(size=(2, P, Hkv, D))
+    ks, vs = g.normal(size=(R, S, Hkv, D)), g.normal(size=(R, S, Hkv, D))
+    off, pl, sl = [0, 2, 3], [5, 0], [0, 4, 1]
+    out, lse = oracle.prefix_attention(q, kp, vp, pl, ks, vs, sl, off, 0.3)
+    # one key: its value, and its score
+    assert np.allclose(out[2, 3], vs[2, 0, 1], atol=1e-15)
+    assert np.allclose(lse[2, 3], 0.3 * q[2, 3] @ ks[2, 0, 1], atol=1e-15)
+    # scale 0: the mean of the values
+    out, lse = oracle.prefix_attention(q, kp, vp, pl, ks, vs, sl, off, 0.0)
+    assert np.allclose(out[1, 0], np.concatenate([vp[0, :, 0], vs[1, :, 0]]).mean(0))
+    assert np.allclose(lse[1], np.log(9.0))
+    # a key moved from the prefix to the suffix changes nothing
+    a = oracle.prefix_attention(q[:1], kp, vp, [5], ks, vs, [1], [0, 1], 0.7)
+    ks2, vs2 = ks.copy(), vs.copy()
+    ks2[0, 1], vs2[0, 1] = kp[0, 4], vp[0, 4]
+    b = oracle.prefix_attention(q[:1], kp, vp, [4], ks2, vs2, [2], [0, 1], 0.7)
+    assert np.allclose(a[0], b[0], atol=1e-14) and np.allclose(a[1], b[1], atol=1e-14)
+    # no key at all
+    a = oracle.prefix_attention(q[:1], kp, vp, [0], ks, vs, [0], [0, 1], 0.7)
+    assert not a[0].any() and (a[1] == -np.inf).all()
