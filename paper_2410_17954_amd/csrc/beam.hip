@@ -12,6 +12,9 @@
 #include "moeflow_decode.h"
 #include "common.h"
 #include "buffers.h"
+#include "rows.h"
+
+#include <float.h>
 
 #include <algorithm>
 
@@ -21,25 +24,26 @@ namespace {
 constexpr int kSelThreads = 256;
 constexpr int kSelWaves = kSelThreads / kWave;
 constexpr int kSelMaxBeams = 32, kSelMaxOut = 64;
-constexpr int kSelChunk = 8192;                  // largest chunk of a row
 constexpr int kMergeThreads = 512;
-constexpr int kMergeLists = 4096 + kSelMaxBeams; // K * ceil(V / 8192) for K * V <= 2^25
+constexpr int kMergeCopy = 4096;                 // keys that a merge keeps in LDS
+constexpr int kMergeLists = 4096 + kSelMaxBeams; // lists of a request, keys that reach a threshold
 
 struct SelLayout {
   size_t stat, val, idx, total;
-  int64_t chunks;
+  int64_t chunks;                                // of a row, a block each
   int ept;                                       // logits a thread takes
 };
 
-// Elements of a thread: 32, or 8 while the grid of the larger chunks would leave
-// compute units idle.
+// 64, or 8 while longer chunks would leave compute units idle and a merge can take
+// the lists.
 SelLayout sel_layout(int64_t B, int32_t K, int64_t V, int32_t n_out) {
   SelLayout s{};
-  s.ept = B * K * ceil_div(V, kSelChunk) < 256 && K * ceil_div(V, kSelChunk / 4) <= kMergeLists ? 8 : 32;
+  s.ept = B * K * ceil_div(V, kSelThreads * 64) < 256 &&
+          K * ceil_div(V, kSelThreads * 8) <= kMergeLists ? 8 : 64;
   s.chunks = ceil_div(V, (int64_t)s.ept * kSelThreads);
   const size_t lists = (size_t)(B * K * s.chunks);
   size_t o = 0;
-  s.stat = o;                                    // {max, sum} of a chunk, double
+  s.stat = o;                                    // {ref, sum of exp(z - ref)} of a chunk, double
   o = align_up(o + lists * 16, 256);
   s.val = o;                                     // the chunk's best logits, descending
   o = align_up(o + lists * n_out * 4, 256);
@@ -50,18 +54,8 @@ SelLayout sel_layout(int64_t B, int32_t K, int64_t V, int32_t n_out) {
 }
 
 template <typename V>
-__device__ __forceinline__ bool ahead(V a, int64_t ai, V b, int64_t bi) {
+__device__ __forceinline__ bool ahead(V a, int32_t ai, V b, int32_t bi) {
   return a > b || (a == b && ai < bi);
-}
-
-__device__ __forceinline__ float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-  return v;
-}
-
-__device__ __forceinline__ int wave_min(int v) {
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, kWave));
-  return v;
 }
 
 // 16 bytes from an address that is only element-aligned.
@@ -70,8 +64,7 @@ struct __attribute__((packed, aligned(2))) Bytes16 { uint32_t w[4]; };
 template <typename Tv> struct LogitVec;
 template <> struct LogitVec<uint16_t> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void load(const uint16_t* p, float* out) {
-    const Bytes16 b = *reinterpret_cast<const Bytes16*>(p);
+  static __device__ __forceinline__ void unpack(const Bytes16& b, float* out) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       out[2 * i] = __uint_as_float(b.w[i] << 16);
@@ -82,149 +75,255 @@ template <> struct LogitVec<uint16_t> {
 };
 template <> struct LogitVec<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void load(const float* p, float* out) {
-    const Bytes16 b = *reinterpret_cast<const Bytes16*>(p);
+  static __device__ __forceinline__ void unpack(const Bytes16& b, float* out) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = __uint_as_float(b.w[i]);
   }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
 
-// One block: logits [c0, c0 + chunk) of row r in registers.
-//   1. chunk maximum and sum of exp (float32 terms, at most EPT of them added in
-//      float32, the rest in float64);
-//   2. per wave, the n-th largest of its lanes' best keys; the largest of these
-//      over the waves is a lower bound T of the chunk's n-th key, and at most
-//      n lanes of a wave hold keys from T on;
-//   3. keys from T on go to LDS (at most n * EPT a wave) and the n best of them
-//      are ranked by counting.
+// Over a wave: m, the largest value; t, the smallest of the largest values of
+// groups of 2^g neighbouring lanes.
+__device__ __forceinline__ void group_extremes(float v, int g, float& m, float& t) {
+  m = t = v;
+  auto step = [&](float om, float ot, int level) {
+    m = fmaxf(m, om);
+    t = level < g ? m : fminf(t, ot);
+  };
+  step(dpp<0xB1>(m), dpp<0xB1>(t), 0);
+  step(dpp<0x4E>(m), dpp<0x4E>(t), 1);
+  step(dpp<0x141>(m), dpp<0x141>(t), 2);
+  step(dpp<0x140>(m), dpp<0x140>(t), 3);
+  step(__shfl_xor(m, 16, kWave), __shfl_xor(t, 16, kWave), 4);
+  step(__shfl_xor(m, 32, kWave), __shfl_xor(t, 32, kWave), 5);
+}
+
+// One block: a chunk of a row in registers.
+//   1. T, the smallest of the largest logits of at least n groups of lanes (4 to
+//      64 of them): a lower bound of the chunk's n-th logit, since every group
+//      holds one from T on;
+//   2. sum of exp (float32 terms, at most 32 of them added in float32, the rest
+//      in float64);
+//   3. logits from T on, some three times n of them however long the chunk, go to
+//      LDS and are ranked by counting.
+// Where a wave holds more than kSelPart of them (equal logits, sorted ones), n
+// rounds over the registers pick the best after the one before instead.
+// What bounds it is instructions, not HBM: 7 a logit (and an exponential, which
+// counts four) and some 400 a wave and chunk, hence long chunks (64 requests of 8
+// beams over 128000 bf16 logits: chunks of 8192 63 us, of 16384 53; blocks that
+// walk over several with the next one's loads in flight 61).
+constexpr int kSelPart = 128;
+
 template <typename Tv, int EPT>
-__global__ void __launch_bounds__(kSelThreads)
+__global__ void __launch_bounds__(kSelThreads, EPT == 64 ? 4 : 8)
 beam_rows_kernel(const Tv* __restrict__ logits, int64_t V, const int32_t* __restrict__ finished,
-                 int n, double2* __restrict__ stat, float* __restrict__ out_val,
+                 int n, int group, double2* __restrict__ stat, float* __restrict__ out_val,
                  int32_t* __restrict__ out_idx) {
   using LV = LogitVec<Tv>;
   constexpr int VE = LV::N, NV = EPT / VE;
-  extern __shared__ float s_val[];               // n * EPT * waves values, then as many tokens
-  int32_t* const s_idx = reinterpret_cast<int32_t*>(s_val + (size_t)n * EPT * kSelWaves);
+  __shared__ float s_val[kSelWaves * kSelPart];
+  __shared__ int32_t s_idx[kSelWaves * kSelPart];
   __shared__ float w_max[kSelWaves], w_thr[kSelWaves];
-  __shared__ int w_thr_idx[kSelWaves];
   __shared__ double w_sum[kSelWaves];
-  __shared__ int s_count;
+  __shared__ float w_best[kSelWaves];
+  __shared__ int32_t w_idx[kSelWaves], w_count[kSelWaves];
   const int64_t row = blockIdx.y;
+  if (finished && finished[row] != 0) return;    // its lists are not read
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  // register e: token c0 + place(e) of the chunk at c0, below 2^25
+  auto place = [&](int e) { return ((e / VE) * kSelThreads + (int)threadIdx.x) * VE + e % VE; };
   const int64_t list = row * gridDim.x + blockIdx.x;
-  if (finished && finished[row] != 0) return;    // its list is not read
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
   const int64_t c0 = (int64_t)blockIdx.x * EPT * kSelThreads;
-  const Tv* const base = logits + row * V;
+  const int left = (int)min(V - c0, (int64_t)EPT * kSelThreads);
+  const Tv* const base = logits + row * V + c0;
   float z[EPT];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int64_t at = c0 + ((int64_t)j * kSelThreads + threadIdx.x) * VE;
-    if (at + VE <= V) {
-      LV::load(base + at, z + j * VE);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VE; ++i) z[j * VE + i] = at + i < V ? LV::one(base + at + i) : -INFINITY;
-    }
+    const int at = place(j * VE);
+    Bytes16 raw = {};
+    if (at + VE <= left) raw = *reinterpret_cast<const Bytes16*>(base + at);
+    LV::unpack(raw, z + j * VE);
   }
-  auto token = [&](int e) {                      // of register e: below 2^25
-    return (int)(c0 + ((int64_t)(e / VE) * kSelThreads + threadIdx.x) * VE + e % VE);
-  };
-  if (threadIdx.x == 0) s_count = 0;
-
-  // the lane's best key: the first of its largest numbers (its tokens ascend)
-  float best = -INFINITY;
+  if (left < EPT * kSelThreads) {                // the row's end: at most one vector is cut
 #pragma unroll
-  for (int e = 0; e < EPT; ++e) best = fmaxf(best, z[e]);
-  int best_idx = 0x7fffffff;
+    for (int j = 0; j < NV; ++j) {
+      const int at = place(j * VE);
+      if (at + VE > left)
 #pragma unroll
-  for (int e = EPT - 1; e >= 0; --e) best_idx = z[e] == best ? token(e) : best_idx;
-  float m = wave_max(best);
-  if (lane == 0) w_max[wave] = m;
-
-  // n-th largest of the lanes' keys: n times the largest leaves
-  float left = best, thr = -INFINITY;
-  int thr_idx = 0x7fffffff;
-  for (int j = 0; j < n; ++j) {
-    const float top = j == 0 ? m : wave_max(left);
-    thr = top;
-    if (top == -INFINITY) break;
-    uint64_t at = ballot(left == top);
-    int first;
-    if (at & (at - 1)) {                         // equal values: the lowest token
-      first = wave_min(left == top ? best_idx : 0x7fffffff);
-    } else {
-      first = __builtin_amdgcn_readlane(best_idx, __ffsll((unsigned long long)at) - 1);
-    }
-    thr_idx = first;
-    if (left == top && best_idx == first) left = -INFINITY;
-  }
-  if (lane == 0) {
-    w_thr[wave] = thr;
-    w_thr_idx[wave] = thr_idx;
-  }
-  __syncthreads();
+        for (int i = 0; i < VE; ++i) z[j * VE + i] = -INFINITY;
+      if (at < left && at + VE > left) {
 #pragma unroll
-  for (int w = 0; w < kSelWaves; ++w) m = fmaxf(m, w_max[w]);
-  thr = w_thr[0];
-  thr_idx = w_thr_idx[0];
-#pragma unroll
-  for (int w = 1; w < kSelWaves; ++w)
-    if (ahead(w_thr[w], w_thr_idx[w], thr, thr_idx)) {
-      thr = w_thr[w];
-      thr_idx = w_thr_idx[w];
-    }
-
-  // sum of exp(z - m); a chunk of -inf adds nothing, NaN and +inf make it NaN
-  const float shift = m == -INFINITY ? 0.f : m;
-  float part = 0.f;
-#pragma unroll
-  for (int e = 0; e < EPT; ++e)
-    part += __builtin_amdgcn_exp2f((z[e] - shift) * 1.4426950408889634f);
-  const double wsum = wave_sum((double)part);
-  if (lane == 0) w_sum[wave] = wsum;
-
-  const int cap = n * EPT * kSelWaves;
-  if (best > thr || (best == thr && best_idx <= thr_idx)) {
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const bool in = z[e] > -INFINITY && (z[e] > thr || (z[e] == thr && token(e) <= thr_idx));
-      if (in) {
-        const int at = atomicAdd(&s_count, 1);
-        if (at < cap) {
-          s_val[at] = z[e];
-          s_idx[at] = token(e);
-        }
+        for (int i = 0; i < VE - 1; ++i)
+          if (at + i < left) z[j * VE + i] = LV::one(base + at + i);
       }
     }
   }
+  float best = -INFINITY;                        // a NaN is no maximum
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) best = fmaxf(best, z[e]);
+  float m, thr;
+  group_extremes(best, group, m, thr);
+  if (lane == 0) {
+    w_max[wave] = m;
+    w_thr[wave] = thr;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    m = fmaxf(m, w_max[w]);
+    thr = fminf(thr, w_thr[w]);
+  }
+
+  // sum of exp(z - m) as 2^(z L - m L): one fma, whose rounding is that of the
+  // small result; m L is rounded first and L is log2 e rounded, so what is summed
+  // is exp(z - ref) up to (z - m) (1 - ln 2 L), with ref below. Where m L overflows
+  // (masks of the lowest number) and for a chunk of -inf, which adds nothing, the
+  // difference is taken first; NaN and +inf make the sum NaN.
+  constexpr float L = 1.4426950408889634f;
+  constexpr int PART = EPT < 32 ? EPT : 32;
+  const bool plain = !(fabsf(m) < 1e38f);
+  const float shift = plain ? (m == -INFINITY ? 0.f : m) : m * L;
+  double dsum = 0.0;
+#pragma unroll
+  for (int e0 = 0; e0 < EPT; e0 += PART) {
+    float part = 0.f;
+    if (plain) {
+#pragma unroll
+      for (int e = e0; e < e0 + PART; ++e) part += __builtin_amdgcn_exp2f((z[e] - shift) * L);
+    } else {
+#pragma unroll
+      for (int e = e0; e < e0 + PART; ++e) part += __builtin_amdgcn_exp2f(fmaf(z[e], L, -shift));
+    }
+    dsum += (double)part;
+  }
+  dsum = wave_sum(dsum);
+  if (lane == 0) w_sum[wave] = dsum;
+
+  thr = fmaxf(thr, -FLT_MAX);                    // -inf is no candidate
+  float* const mine = s_val + wave * kSelPart;
+  int32_t* const mine_idx = s_idx + wave * kSelPart;
+  int found = 0;                                 // the wave's, all of them
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) {
+    const uint64_t in = ballot(z[e] >= thr);
+    if (in == 0) continue;
+    const int at = found + __popcll(in & lanemask_lt());
+    if (z[e] >= thr && at < kSelPart) {
+      mine[at] = z[e];
+      mine_idx[at] = place(e);
+    }
+    found += __popcll(in);
+  }
+  if (lane == 0) w_count[wave] = found;
   __syncthreads();
   if (threadIdx.x == 0) {
     double t = w_sum[0];
     for (int w = 1; w < kSelWaves; ++w) t += w_sum[w];
-    stat[list] = make_double2((double)m, t);
+    // 2^(m L - shift) = exp(m - ref)
+    const double ref = (double)m + ((double)shift - (double)m * (double)L) * 0.6931471805599453;
+    stat[list] = make_double2(plain ? (double)m : ref, t);
   }
-  const int c = min(s_count, cap);
-  for (int q = threadIdx.x; q < c; q += kSelThreads) {
-    const float v = s_val[q];
-    const int i = s_idx[q];
-    int rank = 0;
-    for (int o = 0; o < c; ++o) rank += ahead(s_val[o], s_idx[o], v, i);
-    if (rank < n) {
-      out_val[list * n + rank] = v;
-      out_idx[list * n + rank] = i;
+  float* const val = out_val + list * n;
+  int32_t* const idx = out_idx + list * n;
+  int most = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    most = max(most, w_count[w]);
+    total += w_count[w];
+  }
+  if (most <= kSelPart) {
+    // a wave's keys against all: lanes 4 apart share a key, a wave's part each
+    for (int q0 = 0; q0 < found; q0 += kWave / kSelWaves) {
+      const int q = q0 + lane / kSelWaves, w = lane % kSelWaves;
+      const bool ok = q < found;
+      const float v = ok ? mine[q] : 0.f;
+      const int i = ok ? mine_idx[q] : 0;
+      const int end = ok ? w_count[w] : 0;
+      int r = 0;
+#pragma unroll 4
+      for (int o = 0; o < end; ++o) r += ahead(s_val[w * kSelPart + o], s_idx[w * kSelPart + o], v, i);
+      r += dpp<0xB1>(r);
+      r += dpp<0x4E>(r);
+      if (ok && w == 0 && r < n) {
+        val[r] = v;
+        idx[r] = (int)c0 + i;
+      }
     }
+    for (int q = total + threadIdx.x; q < n; q += kSelThreads) {
+      val[q] = -INFINITY;
+      idx[q] = -1;
+    }
+    return;
   }
-  for (int q = c + threadIdx.x; q < n; q += kSelThreads) {
-    out_val[list * n + q] = -INFINITY;
-    out_idx[list * n + q] = -1;
+  float pv = INFINITY;                           // the key before: everything comes after it
+  int pi = -1;
+  for (int j = 0; j < n; ++j) {                  // more than n numbers: there is always one left
+    float bv = -INFINITY;
+    int bi = 0x7fffffff;
+    int at0 = (int)threadIdx.x * VE;             // opaque, or all places live in registers
+    asm volatile("" : "+v"(at0));
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int at = at0 + (e / VE) * kSelThreads * VE + e % VE;
+      // a lane's places ascend: the first of its largest stays
+      const bool after = z[e] < pv || (z[e] == pv && at > pi);
+      if (after && (z[e] > bv || bi == 0x7fffffff)) {
+        bv = z[e];
+        bi = at;
+      }
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+      const float ov = __shfl_xor(bv, o, kWave);
+      const int oi = __shfl_xor(bi, o, kWave);
+      if (ahead(ov, oi, bv, bi)) {
+        bv = ov;
+        bi = oi;
+      }
+    }
+    if (lane == 0) {
+      w_best[wave] = bv;
+      w_idx[wave] = bi;
+    }
+    __syncthreads();
+    pv = w_best[0];
+    pi = w_idx[0];
+#pragma unroll
+    for (int w = 1; w < kSelWaves; ++w)
+      if (ahead(w_best[w], w_idx[w], pv, pi)) {
+        pv = w_best[w];
+        pi = w_idx[w];
+      }
+    if (threadIdx.x == 0) {
+      val[j] = pv;
+      idx[j] = (int)c0 + pi;
+    }
+    __syncthreads();                             // w_best is rewritten next
   }
+}
+
+// rank[i] = keys ahead of key i, for i < count, by the whole block: as many threads
+// share a key as there are. rank is zero on entry; ends with a barrier.
+__device__ __forceinline__ void merge_ranks(const double* key, const int32_t* pos, int count,
+                                            int32_t* rank) {
+  const int per = max(1, kMergeThreads / max(count, 1));
+  for (int q = threadIdx.x; q < count * per; q += kMergeThreads) {
+    const int i = q % count, p = q / count;
+    const double c = key[i];
+    const int32_t at = pos[i];
+    int r = 0;
+#pragma unroll 4
+    for (int o = count * p / per; o < count * (p + 1) / per; ++o) r += ahead(key[o], pos[o], c, at);
+    if (r) atomicAdd(&rank[i], r);
+  }
+  __syncthreads();
 }
 
 // One block per request: the rows' log-sum-exp, then the n best of the lists.
 // The n-th largest of the lists' first keys is a lower bound of the n-th key,
-// and fewer than n lists hold keys above it: at most n * n keys are ranked.
+// and fewer than n lists hold keys above it: at most n * n keys are ranked. Such
+// a block is bound by its loads' latency: the lists go to LDS beside the rows'
+// sums where they fit.
 __global__ void __launch_bounds__(kMergeThreads)
 beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* __restrict__ scores,
                   const int32_t* __restrict__ finished, int64_t eos,
@@ -233,29 +332,51 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* __restrict__
                   int32_t* __restrict__ token, float* __restrict__ out_scores,
                   int32_t* __restrict__ out_finished) {
   __shared__ double s_key[kMergeLists];          // first keys, then the keys to rank
-  __shared__ int32_t s_pos[kMergeLists];         // beam * V + token, below 2^25
+  __shared__ int32_t s_pos[kMergeLists];         // beam << 25 | token: in the order of both
+  __shared__ int32_t s_rank[kMergeLists];
+  __shared__ float c_val[kMergeCopy];
+  __shared__ int32_t c_idx[kMergeCopy];
   __shared__ double s_off[kSelMaxBeams];         // score - lse, or the score of a finished beam
   __shared__ int s_done[kSelMaxBeams];
   __shared__ double s_thr;
-  __shared__ int s_thr_pos, s_count;
+  __shared__ int32_t s_thr_pos;
+  __shared__ int s_count;
   const int64_t b = blockIdx.x;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int lists = K * chunks, keys = lists * n;
+  const float* const g_val = val + b * keys;
+  const int32_t* const g_idx = idx + b * keys;
+  const bool copied = keys <= kMergeCopy;
+  float fv[kMergeCopy / kMergeThreads];
+  int32_t fi[kMergeCopy / kMergeThreads];
+  if (copied) {
+#pragma unroll
+    for (int i = 0; i < kMergeCopy / kMergeThreads; ++i) {
+      const int q = threadIdx.x + i * kMergeThreads;
+      fv[i] = q < keys ? g_val[q] : 0.f;
+      fi[i] = q < keys ? g_idx[q] : -1;
+    }
+  }
   if (threadIdx.x == 0) {
     s_thr = -INFINITY;
     s_thr_pos = 0x7fffffff;
     s_count = 0;
   }
+  for (int l = threadIdx.x; l < kMergeLists; l += kMergeThreads) s_rank[l] = 0;
   // a row's chunks are added lane by lane, then over the lanes: a fixed order
   for (int k = wave; k < K; k += kMergeThreads / kWave) {
     const int64_t row = b * K + k;
+    const double2* const st = stat + row * chunks;
+    double2 first = make_double2(-INFINITY, 0.0);
+    if (lane < chunks) first = st[lane];
     const int done = finished && finished[row] != 0;
     double off = (double)scores[row];
     if (!done) {
-      double m = -INFINITY, t = 0.0;
-      for (int c = lane; c < chunks; c += kWave) m = fmax(m, stat[row * chunks + c].x);
+      double m = first.x, t = 0.0;
+      for (int c = lane + kWave; c < chunks; c += kWave) m = fmax(m, st[c].x);
       for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o, kWave));
       for (int c = lane; c < chunks; c += kWave) {
-        const double2 s = stat[row * chunks + c];
+        const double2 s = c == lane ? first : st[c];
         t += s.x == -INFINITY ? s.y : s.y * exp(s.x - m);   // 0, or the NaN it holds
       }
       t = wave_sum(t);
@@ -266,57 +387,64 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* __restrict__
       s_done[k] = done;
     }
   }
+  if (copied) {
+#pragma unroll
+    for (int i = 0; i < kMergeCopy / kMergeThreads; ++i) {
+      const int q = threadIdx.x + i * kMergeThreads;
+      if (q < keys) {
+        c_val[q] = fv[i];
+        c_idx[q] = fi[i];
+      }
+    }
+  }
   __syncthreads();
-  const int lists = K * chunks;
-  // key j of list l; the single key of a finished beam is in its first list
-  auto key = [&](int l, int j, double& c, int32_t& pos) {
-    const int k = l / chunks;
+  // key j of list l of beam k; the single key of a finished beam is in its first list
+  auto key = [&](int k, int l, int j, double& c, int32_t& pos) {
     c = -INFINITY;
     pos = 0x7fffffff;
-    int64_t t = -1;
+    int t = -1;
     if (s_done[k]) {
-      if (l % chunks == 0 && j == 0) {
+      if (l == k * chunks && j == 0) {
         c = s_off[k];
-        t = eos;
+        t = (int)eos;
       }
     } else {
-      const int64_t at = ((b * K) * chunks + l) * n + j;
-      t = idx[at];
-      if (t >= 0) c = (double)val[at] + s_off[k];
+      const int at = l * n + j;
+      t = copied ? c_idx[at] : g_idx[at];
+      if (t >= 0) c = (double)(copied ? c_val[at] : g_val[at]) + s_off[k];
     }
     if (t < 0 || !(c > -INFINITY)) c = -INFINITY;          // NaN too
-    else pos = (int32_t)(k * V + t);
+    else pos = k << 25 | t;
   };
   for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
     double c;
     int32_t pos;
-    key(l, 0, c, pos);
+    key(l / chunks, l, 0, c, pos);
     s_key[l] = c;
     s_pos[l] = pos;
   }
   __syncthreads();
   if (lists > n) {
-    for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
-      const double c = s_key[l];
-      const int32_t pos = s_pos[l];
-      if (!(c > -INFINITY)) continue;
-      int rank = 0;
-      for (int o = 0; o < lists; ++o) rank += ahead(s_key[o], s_pos[o], c, pos);
-      if (rank == n - 1) {                       // at most one list
-        s_thr = c;
-        s_thr_pos = pos;
+    merge_ranks(s_key, s_pos, lists, s_rank);
+    for (int l = threadIdx.x; l < lists; l += kMergeThreads)
+      if (s_rank[l] == n - 1 && s_key[l] > -INFINITY) {    // at most one list
+        s_thr = s_key[l];
+        s_thr_pos = s_pos[l];
       }
-    }
+    __syncthreads();
+    for (int l = threadIdx.x; l < lists; l += kMergeThreads) s_rank[l] = 0;
   }
-  __syncthreads();
   const double thr = s_thr;
   const int32_t thr_pos = s_thr_pos;
-  // lists of at most n, and at most n of them reach the threshold
-  for (int q = threadIdx.x; q < lists * n; q += kMergeThreads) {
-    double c;
-    int32_t pos;
-    key(q / n, q % n, c, pos);
-    if (c > -INFINITY && (c > thr || (c == thr && pos <= thr_pos))) {
+  // lists of at most n, in descending order, and at most n of them reach the threshold
+  for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
+    const int k = l / chunks;
+    for (int j = 0; j < n; ++j) {
+      double c;
+      int32_t pos;
+      key(k, l, j, c, pos);
+      if (!(c > -INFINITY) || c < thr) break;
+      if (c == thr && pos > thr_pos) continue;
       const int at = atomicAdd(&s_count, 1);
       if (at < kMergeLists) {
         s_key[at] = c;
@@ -332,14 +460,13 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* __restrict__
     out_scores[b * n + at] = c;
     if (out_finished) out_finished[b * n + at] = fin;
   };
+  merge_ranks(s_key, s_pos, count, s_rank);
   for (int q = threadIdx.x; q < count; q += kMergeThreads) {
     const double c = s_key[q];
     const int32_t pos = s_pos[q];
-    int rank = 0;
-    for (int o = 0; o < count; ++o) rank += ahead(s_key[o], s_pos[o], c, pos);
+    const int rank = s_rank[q];
     if (rank < n) {
-      const int k = (int)(pos / V);
-      const int32_t t = (int32_t)(pos % V);
+      const int k = pos >> 25, t = pos & 0x1ffffff;
       put(rank, (int32_t)(b * K + k), t, (float)c, t == eos || s_done[k]);
     }
   }
@@ -499,23 +626,25 @@ extern "C" int moe_beam_select(const void* logits, int32_t dtype, int64_t B, int
   auto* stat = reinterpret_cast<double2*>(ws + lay.stat);
   auto* val = reinterpret_cast<float*>(ws + lay.val);
   auto* idx = reinterpret_cast<int32_t*>(ws + lay.idx);
-  const unsigned lds = (unsigned)(n_out * lay.ept * kSelWaves * 8);
+  // lanes of a group, 2^group: 256 threads hold at least n_out groups
+  int group = 6;
+  while (group > 2 && (kSelThreads >> group) < n_out) --group;
   // rows in slices of the y dimension's limit
   constexpr int64_t kSlice = 32768;
   for (int64_t r0 = 0; r0 < B * K; r0 += kSlice) {
     const dim3 grid((unsigned)lay.chunks, (unsigned)std::min<int64_t>(kSlice, B * K - r0));
     const int32_t* const fin = finished ? finished + r0 : nullptr;
     const int64_t l0 = r0 * lay.chunks;
-#define MOE_ROWS(T, EPT)                                                                   \
-  beam_rows_kernel<T, EPT><<<grid, dim3(kSelThreads), lds, st>>>(                          \
-      static_cast<const T*>(logits) + r0 * V, V, fin, n_out, stat + l0, val + l0 * n_out,  \
+#define MOE_ROWS(T, EPT)                                                                         \
+  beam_rows_kernel<T, EPT><<<grid, dim3(kSelThreads), 0, st>>>(                                  \
+      static_cast<const T*>(logits) + r0 * V, V, fin, n_out, group, stat + l0, val + l0 * n_out, \
       idx + l0 * n_out)
     if (dtype == MOE_BF16) {
       if (lay.ept == 8) MOE_ROWS(uint16_t, 8);
-      else MOE_ROWS(uint16_t, 32);
+      else MOE_ROWS(uint16_t, 64);
     } else {
       if (lay.ept == 8) MOE_ROWS(float, 8);
-      else MOE_ROWS(float, 32);
+      else MOE_ROWS(float, 64);
     }
 #undef MOE_ROWS
     MOE_CHECK_LAUNCH();

@@ -6,6 +6,7 @@ and passes raw pointers and the current HIP stream to the C entry point of the
 same name. All arithmetic of the hot path runs in the library's HIP kernels;
 there is no fallback. If the library has not been built, the first call raises.
 """
+import contextlib
 import ctypes
 import os
 
@@ -714,19 +715,55 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
 
 
 # ----------------------------------------------------------------- decode step
+# These calls are a few microseconds of kernels: the host's share is kept below
+# that (no size query where a workspace is given -- the library checks it -- and
+# no change of device where it is the current one).
+_CURRENT = contextlib.nullcontext()
+
+
 def _one_device(*ts):
-    """Every given tensor contiguous, on one GPU: a context that makes it the
-    current device (its stream is then the one the call goes to)."""
-    _dev(*ts)
-    devs = {t.device for t in ts if t is not None}
-    if len(devs) != 1:
-        raise ValueError("every tensor must be on the same GPU")
-    return _torch().cuda.device(devs.pop())
+    """Every given tensor contiguous, on one GPU: a context in which that is the
+    current device (its current stream is the one the call goes to)."""
+    dev = -1
+    for t in ts:
+        if t is None:
+            continue
+        d = t.get_device()
+        if d < 0:
+            raise ValueError("every tensor must be on the GPU")
+        if not t.is_contiguous():
+            raise ValueError("every tensor must be contiguous")
+        if dev < 0:
+            dev = d
+        elif d != dev:
+            raise ValueError("every tensor must be on the same GPU")
+    cuda = _torch().cuda
+    return _CURRENT if dev == cuda.current_device() else cuda.device(dev)
 
 
 def _want(name, t, shape, dtype):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(stream=None):
+    """The given stream, else the current one of the current device, as an
+    address (without an object for it)."""
+    torch = _torch()
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _scratch(workspace, device, query, *args):
+    """(tensor, bytes): the given workspace, else one of query(*args) bytes."""
+    if workspace is not None:
+        return workspace, workspace.numel() * workspace.element_size()
+    return _workspace(query(*args), device, None)
 
 
 def prefix_attention_workspace(R, G, Hq, Hkv, D, P, S, dtype_code=MOE_BF16):
@@ -774,13 +811,13 @@ def prefix_attention(q, k_prefix=None, v_prefix=None, k_suffix=None, v_suffix=No
             out = torch.empty_like(q) if group_offsets is None else torch.zeros_like(q)
         if lse is None and want_lse:
             lse = torch.full((R, Hq), -float("inf"), dtype=torch.float32, device=q.device)
-        ws, nbytes = _workspace(
-            lib.moe_prefix_attention_workspace(R, G, Hq, Hkv, D, P, S, dt), q.device, workspace)
+        ws, nbytes = _scratch(workspace, q.device, lib.moe_prefix_attention_workspace, R, G, Hq,
+                              Hkv, D, P, S, dt)
         st = lib.moe_prefix_attention(
-            _ptr(q), dt, R, Hq, Hkv, D, _ptr(group_offsets), G, _ptr(k_prefix), _ptr(v_prefix), P,
-            _ptr(prefix_len), _ptr(k_suffix), _ptr(v_suffix), S, _ptr(suffix_len),
-            float(D ** -0.5 if scale is None else scale), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
-            _stream(stream))
+            _addr(q), dt, R, Hq, Hkv, D, _addr(group_offsets), G, _addr(k_prefix), _addr(v_prefix), P,
+            _addr(prefix_len), _addr(k_suffix), _addr(v_suffix), S, _addr(suffix_len),
+            float(D ** -0.5 if scale is None else scale), _addr(out), _addr(lse), _addr(ws), nbytes,
+            _raw_stream(stream))
     _check("moe_prefix_attention", st)
     return out, lse
 
@@ -838,13 +875,12 @@ def layer_decode(x, w_router, w_gate, w_up, w_down, k, bias=None, renormalize=Tr
             topk_w = torch.empty((T, k), dtype=torch.float32, device=dev)
         if incomplete is None and want_incomplete:
             incomplete = torch.empty(T, dtype=torch.int32, device=dev)
-        ws, nbytes = _workspace(lib.moe_layer_decode_workspace(T, H, F, E, k, Fs, dt), dev,
-                                workspace)
-        st = lib.moe_layer_decode(_ptr(x), dt, T, H, _ptr(w_router), E, k, _ptr(bias), bias_mode,
-                                  1 if renormalize else 0, _ptr(w_gate), _ptr(w_up), _ptr(w_down),
-                                  S, F, _ptr(slot_of_expert), _ptr(sg), _ptr(su), _ptr(sd), Fs,
-                                  1 if accumulate else 0, _ptr(y), _ptr(topk_idx), _ptr(topk_w),
-                                  _ptr(incomplete), _ptr(ws), nbytes, _stream(stream))
+        ws, nbytes = _scratch(workspace, dev, lib.moe_layer_decode_workspace, T, H, F, E, k, Fs, dt)
+        st = lib.moe_layer_decode(_addr(x), dt, T, H, _addr(w_router), E, k, _addr(bias), bias_mode,
+                                  1 if renormalize else 0, _addr(w_gate), _addr(w_up), _addr(w_down),
+                                  S, F, _addr(slot_of_expert), _addr(sg), _addr(su), _addr(sd), Fs,
+                                  1 if accumulate else 0, _addr(y), _addr(topk_idx), _addr(topk_w),
+                                  _addr(incomplete), _addr(ws), nbytes, _raw_stream(stream))
     _check("moe_layer_decode", st)
     return y, topk_idx, topk_w, incomplete
 
@@ -883,12 +919,12 @@ def beam_select(logits, scores, n_out=None, finished=None, eos=None, parent=None
         out_scores = new(out_scores, torch.float32)
         if eos is not None:
             out_finished = new(out_finished, torch.int32)
-        ws, nbytes = _workspace(lib.moe_beam_select_workspace(B, K, V, n_out), logits.device,
-                                workspace)
-        st = lib.moe_beam_select(_ptr(logits), dt, B, K, V, _ptr(scores), _ptr(finished),
-                                 -1 if eos is None else int(eos), n_out, _ptr(parent), _ptr(token),
-                                 _ptr(out_scores), _ptr(out_finished), _ptr(ws), nbytes,
-                                 _stream(stream))
+        ws, nbytes = _scratch(workspace, logits.device, lib.moe_beam_select_workspace, B, K, V,
+                              n_out)
+        st = lib.moe_beam_select(_addr(logits), dt, B, K, V, _addr(scores), _addr(finished),
+                                 -1 if eos is None else int(eos), n_out, _addr(parent), _addr(token),
+                                 _addr(out_scores), _addr(out_finished), _addr(ws), nbytes,
+                                 _raw_stream(stream))
     _check("moe_beam_select", st)
     return parent, token, out_scores, out_finished
 
@@ -926,7 +962,7 @@ def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None
         if err is None:
             err = torch.zeros(1, dtype=torch.int32, device=dev)
         ptrs = (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches])
-        st = lib.moe_beam_reorder(ptrs, len(caches), L, B, K, S, unit, _ptr(parent), _ptr(lens),
-                                  _ptr(new_lens), _ptr(err), _stream(stream))
+        st = lib.moe_beam_reorder(ptrs, len(caches), L, B, K, S, unit, _addr(parent), _addr(lens),
+                                  _addr(new_lens), _addr(err), _raw_stream(stream))
     _check("moe_beam_reorder", st)
     return new_lens, err

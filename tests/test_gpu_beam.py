@@ -130,6 +130,23 @@ def test_select_unaligned_rows_and_reused_buffers():
     assert np.array_equal(to_host(outs[2]), rd)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 16, 17, 64])
+def test_select_masked_to_few_and_equal_chunks(n, dtype):
+    # constrained decoding: all but a few tokens at the lowest number; whole
+    # chunks of one value, and chunks sorted either way
+    V = 20000
+    low = np.finfo(np.float32).min if dtype == "f32" else -3.3895313892515355e38
+    z = np.full((1, 4, V), low, np.float32)
+    z[0, 0, [3, 9000, 19999]] = [1.0, 2.0, 1.5]
+    z[0, 1] = 0.25
+    z[0, 2] = np.linspace(-2, 2, V)
+    z[0, 3] = np.linspace(2, -2, V)
+    bits = synth.bf16_bits(z) if dtype == "bf16" else z
+    s = np.array([[0.0, 3.5, 2.1, 1.3]], np.float32)
+    _check_select(to_dev(bits), synth.values(bits) if dtype == "bf16" else z.astype(np.float64), s, n)
+
+
 def test_select_many_requests():
     # more rows than one launch's second dimension takes
     g = np.random.default_rng(5)
