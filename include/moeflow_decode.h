@@ -51,8 +51,8 @@ extern "C" {
  *                NULL when P == S == 0)
  * Limits: R >= 1, 1 <= G <= R, Hq a multiple of Hkv, D a multiple of 8 up to
  *   256, P, S < 2^31, Hkv * D * element size < 2^26, tensors of dtype on 16
- *   bytes, scale finite. Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED,
- *   MOE_ERR_WORKSPACE, MOE_ERR_HIP.
+ *   bytes, scale finite (below 1e-37 it counts as 0). Errors: MOE_ERR_ARG,
+ *   MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_prefix_attention_workspace(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D,
                                       int64_t P, int64_t S, int32_t dtype);

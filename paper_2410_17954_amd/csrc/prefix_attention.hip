@@ -28,7 +28,7 @@
 namespace moe {
 namespace {
 
-constexpr int kPaThreads = 256, kPaWaves = kPaThreads / kWave;
+constexpr int kJoinThreads = 256;
 constexpr uint32_t kPastEnd = 0x7ffffff0u;       // no buffer here is as long
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -37,7 +37,9 @@ struct PaArgs {
   const int32_t *group_offsets, *prefix_len, *suffix_len;
   int64_t R, G, P, S;
   int Hq, Hkv, D, nq;                            // nq: query heads of a key head
-  float scale2;                                  // scale * log2 e
+  float scale2;                                  // |scale| log2 e
+  uint32_t keep, flip;                           // q & keep ^ flip: no bits where scale is 0,
+                                                 // signs turned where it is negative
   int splits_p, splits_s;                        // of a prefix, of a suffix
   int64_t blocks_p;                              // blocks of the prefixes, which come first
   int64_t slots_p;                               // row tiles of the prefixes (upper bound)
@@ -63,15 +65,19 @@ struct PaJob {
 // different groups never meet, and a slot's group is found without a scan.
 template <typename Tv, int BM>
 __device__ __forceinline__ bool find_job(const PaArgs& a, int64_t block, PaJob& j) {
+  // Block b runs on XCD b % 8. Units (row tile, split) are dealt to the XCDs and an
+  // XCD takes all heads of one: heads lie next to each other in a cache, and an XCD
+  // that read one head only would load few channels of its L2 (268 MB of keys and
+  // values of 8 heads 73 us, 4 rows).
   int64_t len;
-  if (block < a.blocks_p) {
-    // slots of one head and split are neighbours eight apart: blocks of one
-    // XCD share the keys they read in its L2
-    const int64_t slot = block / 8 % a.slots_p;
-    const int64_t hs = block / (8 * a.slots_p) * 8 + block % 8;
-    if (hs >= (int64_t)a.Hkv * a.splits_p) return false;
-    j.h = (int)(hs % a.Hkv);
-    j.split = (int)(hs / a.Hkv);
+  const bool prefix = block < a.blocks_p;
+  if (!prefix) block -= a.blocks_p;
+  const int64_t v = block / (8 * a.Hkv) * 8 + block % 8;
+  j.h = (int)(block / 8 % a.Hkv);
+  if (prefix) {
+    const int64_t slot = v / a.splits_p;
+    j.split = (int)(v % a.splits_p);
+    if (slot >= a.slots_p) return false;
     int64_t lo = 0, hi = a.G;                    // last group whose first slot is <= slot
     while (hi - lo > 1) {
       const int64_t mid = (lo + hi) / 2;
@@ -94,13 +100,9 @@ __device__ __forceinline__ bool find_job(const PaArgs& a, int64_t block, PaJob& 
     j.hi = min(len, j.lo + per);
     return true;
   }
-  block -= a.blocks_p;
-  j.split = (int)(block % a.splits_s);
-  block /= a.splits_s;
-  j.h = (int)(block % a.Hkv);
-  block /= a.Hkv;
-  const int tile = (int)(block % a.tiles_s);
-  j.row0 = block / a.tiles_s;
+  j.split = (int)(v % a.splits_s);
+  const int tile = (int)(v / a.splits_s % a.tiles_s);
+  j.row0 = v / a.splits_s / a.tiles_s;
   if (j.row0 >= a.R || j.row0 < group_row(a, 0) || j.row0 >= group_row(a, a.G)) return false;
   j.m0 = tile * 16;
   j.m_n = min(a.nq - j.m0, 16);
@@ -129,7 +131,8 @@ typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 // One step of a wave: KT tiles of 16 keys. DP: the dimension padded to whole
 // lines of 128 bytes; 16-byte chunks past D are zeros. Rows are loaded as 8 keys
-// x 128 bytes an instruction and become MFMA operands by a swap between lanes l
+// x 128 bytes an instruction, non-temporal (a block is mostly the only reader of its
+// keys: 4 rows behind 65536 keys 55 us with the hint off, 49), and become MFMA operands by a swap between lanes l
 // and l ^ 8 (ror8_into): operand 2l + h of lane (key r, q) holds the line's chunk
 // 4h + q.
 template <typename Tv, int DP>
@@ -157,7 +160,7 @@ struct PaCore {
 #pragma unroll
       for (int l = 0; l < LN; ++l) {
         const uint32_t off = (uint32_t)(g * 8 + (lane & 7)) * stride + (l * 8 + c) * 16;
-        r.v[g][l] = buf_load16<false>(rs, (l * 8 + c) * VE < D ? off : kPastEnd, 0);
+        r.v[g][l] = buf_load16<true>(rs, (l * 8 + c) * VE < D ? off : kPastEnd, 0);
       }
   }
   static __device__ __forceinline__ void mfma(f32x4_t& c, const u32x4_t& x, const u32x4_t& y) {
@@ -263,7 +266,85 @@ __device__ __forceinline__ void lds_fence() {    // LDS of one wave: program ord
   asm volatile("" ::: "memory");
 }
 
-template <typename Tv, int DP, int MT>
+// Scores -> softmax numerators of one step, in place, for MT column tiles; keys
+// from hi - key on are none. m: reference of the numerators 2^(s scale2 - m), raised
+// (and l and o rescaled) only where a score exceeds it by more than kSlack, so that
+// most steps rescale nothing and numerators stay below 2^kSlack. One branch for all
+// tiles: the rest of a step is straight code.
+constexpr float kSlack = 8.f;
+
+template <int MT, int KT, int DT>
+__device__ __forceinline__ void pa_softmax(f32x4_t (&s)[MT][KT], float (&m)[MT], float (&l)[MT],
+                                           f32x4_t (&o)[MT][DT], float scale2, int keys) {
+  const int q4 = lane_id() >> 4;
+  if (keys < 16 * KT) {                          // scale2 > 0: no weight
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * kt + 4 * q4 + e >= keys) s[i][kt][e] = -INFINITY;
+  }
+  float mx[MT];
+  bool raise = false;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    mx[i] = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx[i] = fmaxf(mx[i], s[i][kt][e]);
+    mx[i] = quad_max(mx[i]) * scale2;
+    raise = raise || mx[i] > m[i] + kSlack;
+  }
+  if (ballot(raise)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const float to = mx[i] > m[i] + kSlack ? mx[i] : m[i];
+      const float f = to == m[i] ? 1.f : __builtin_amdgcn_exp2f(m[i] - to);   // 0 from -inf
+      m[i] = to;
+      l[i] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[i][dt] *= f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const float mu = m[i] == -INFINITY ? 0.f : m[i];         // nothing but -inf so far
+    float sum = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[i][kt][e], scale2, -mu));
+        s[i][kt][e] = p;
+        sum += p;
+      }
+    l[i] += sum;
+  }
+}
+
+// Query operands of MT column tiles from column m0 of the job on; columns past its
+// last and dimensions past D are zeros.
+template <typename C, typename Tv, int MT, typename RowHead>
+__device__ __forceinline__ void pa_queries(u32x4_t (&q)[MT][C::QR], const PaArgs& a, const PaJob& j,
+                                           RowHead&& rowhead, int m0) {
+  const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int m = m0 + 16 * i + r;
+    const Tv* const qr = static_cast<const Tv*>(a.q) + (m < j.m_n ? rowhead(m) : 0) * a.D;
+#pragma unroll
+    for (int s = 0; s < C::QR; ++s) {
+      const int d = (4 * s + q4) * C::VE;
+      q[i][s] = u32x4_t{0, 0, 0, 0};
+      if (m < j.m_n && d < a.D) q[i][s] = (*reinterpret_cast<const u32x4_t*>(qr + d) & a.keep) ^ a.flip;
+    }
+  }
+}
+
+template <typename Tv, int DP, int MT, int W>
 __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* lds,
                                          float (*s_m)[64], float (*s_l)[64]) {
   using C = PaCore<Tv, DP>;
@@ -275,21 +356,12 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
     return (j.row0 + (j.m0 + m) / a.nq) * a.Hq + j.h * a.nq + (j.m0 + m) % a.nq;
   };
   if (j.lo >= j.hi) {                            // no keys: this split adds nothing
-    for (int m = threadIdx.x; m < j.m_n; m += kPaThreads)
+    for (int m = threadIdx.x; m < j.m_n; m += (64 * W))
       a.part_ml[j.split * RH + rowhead(m)] = make_float2(-INFINITY, 0.f);
     return;
   }
   u32x4_t q[MT][C::QR];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = 16 * i + r;
-    const Tv* const qr = static_cast<const Tv*>(a.q) + (m < j.m_n ? rowhead(m) : 0) * a.D;
-#pragma unroll
-    for (int s = 0; s < C::QR; ++s) {
-      const int d = (4 * s + q4) * C::VE;
-      q[i][s] = m < j.m_n && d < a.D ? *reinterpret_cast<const u32x4_t*>(qr + d) : u32x4_t{0, 0, 0, 0};
-    }
-  }
+  pa_queries<C, Tv>(q, a, j, rowhead, 0);
   f32x4_t o[MT][DT];
   float m_run[MT], l_run[MT];
 #pragma unroll
@@ -311,43 +383,12 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
     f32x4_t s[MT][KT];
     C::template scores<MT>(s, q, k);
     C::stage(mine, v);
-    const int64_t next = key + kPaWaves * C::KEYS;
+    const int64_t next = key + W * C::KEYS;
     if (next < j.hi) {
       C::load(k, j.k, next, j.hi, stride, a.D);
       C::load(v, j.v, next, j.hi, stride, a.D);
     }
-    const bool ragged = key + C::KEYS > j.hi;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float t = s[i][kt][e] * a.scale2;
-          if (ragged && key + 16 * kt + 4 * q4 + e >= j.hi) t = -INFINITY;
-          s[i][kt][e] = t;
-          mx = fmaxf(mx, t);
-        }
-      mx = fmaxf(m_run[i], quad_max(mx));
-      const float mu = mx == -INFINITY ? 0.f : mx;         // nothing but -inf so far
-      if (ballot(mx > m_run[i])) {
-        const float alpha = __builtin_amdgcn_exp2f(m_run[i] - mu);
-        l_run[i] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[i][dt] *= alpha;
-        m_run[i] = mx;
-      }
-      float sum = 0.f;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[i][kt][e] = __builtin_amdgcn_exp2f(s[i][kt][e] - mu);
-          sum += s[i][kt][e];
-        }
-      l_run[i] += sum;
-    }
+    pa_softmax(s, m_run, l_run, o, a.scale2, (int)min(j.hi - key, (int64_t)C::KEYS));
     lds_fence();
     C::template values<MT>(o, s, mine);
     lds_fence();
@@ -369,24 +410,22 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
     const int m = 16 * i + r;
     float top = s_m[0][m];
 #pragma unroll
-    for (int w = 1; w < kPaWaves; ++w) top = fmaxf(top, s_m[w][m]);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, s_m[w][m]);
     const float mu = top == -INFINITY ? 0.f : top;
     const float f = __builtin_amdgcn_exp2f(m_run[i] - mu);
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPaWaves; ++w) l += s_l[w][m] * __builtin_amdgcn_exp2f(s_m[w][m] - mu);
+    for (int w = 0; w < W; ++w) l += s_l[w][m] * __builtin_amdgcn_exp2f(s_m[w][m] - mu);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) part[(wave * DT + dt) * kWave + lane] = o[i][dt] * f;
     __syncthreads();
     if (m < j.m_n) {
       const int64_t at = j.split * RH + rowhead(m);
       if (wave == 0 && q4 == 0) a.part_ml[at] = make_float2(top, l);
-#pragma unroll
-      for (int t = 0; t < DT / kPaWaves; ++t) {
-        const int dt = wave * (DT / kPaWaves) + t;
+      for (int dt = wave; dt < DT; dt += W) {
         f32x4_t sum = part[dt * kWave + lane];
 #pragma unroll
-        for (int w = 1; w < kPaWaves; ++w) sum += part[(w * DT + dt) * kWave + lane];
+        for (int w = 1; w < W; ++w) sum += part[(w * DT + dt) * kWave + lane];
         const int d = 16 * dt + 4 * q4;          // D is a multiple of 8
         if (d < a.D) *reinterpret_cast<f32x4_t*>(a.part_o + at * a.D + d) = sum;
       }
@@ -395,64 +434,229 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
   }
 }
 
-// MT: 16-column tiles of a prefix block; suffix blocks have one. The most that
-// leaves every instance without a spilled register; with four, or dimensions
-// past 128, one wave a SIMD has all of them.
-constexpr int pa_max_tiles(int elt, int dp) {
-  return dp == 256 ? 1 : dp == 128 && elt == 4 ? 2 : 4;
-}
-template <typename Tv, int DP, int MT>
-__global__ void __launch_bounds__(kPaThreads, MT == 4 || DP == 256 ? 1 : 2)
-pa_kernel(PaArgs a) {
+// Many columns (a batch behind one prompt): every wave has MT column tiles of its
+// own and goes over all keys of the block, which are staged in LDS for all of them,
+// 32 keys at a time in two buffers; two more steps are in flight in registers. Keys
+// are then loaded once for 16 * MT * W columns, and MFMAs bound the kernel with the
+// exponentials beside them, where waves that split the keys would each wait for
+// their own.
+template <int DP, int MT, int W>
+__device__ __forceinline__ void pa_rows_block(const PaArgs& a, const PaJob& j, char* lds) {
+  using Tv = uint16_t;
   using C = PaCore<Tv, DP>;
-  __shared__ __attribute__((aligned(16))) char lds[kPaWaves * C::kStage];
-  __shared__ float s_m[kPaWaves][64], s_l[kPaWaves][64];
-  static_assert(kPaWaves * C::kStage >= kPaWaves * C::DT * kWave * 16, "O of the waves");
-  PaJob j;
-  if (!find_job<Tv, 16 * MT>(a, blockIdx.x, j)) return;
-  if ((int64_t)blockIdx.x < a.blocks_p) pa_block<Tv, DP, MT>(a, j, lds, s_m, s_l);
-  else pa_block<Tv, DP, 1>(a, j, lds, s_m, s_l);
+  constexpr int KEYS = 32, CH = C::CHUNKS, DT = C::DT;
+  constexpr int NL = (KEYS * CH + 64 * W - 1) / (64 * W);   // 16-byte chunks of K a thread, and of V
+  constexpr int kTile = KEYS * DP * 2;
+  const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t RH = a.R * a.Hq;
+  auto rowhead = [&](int m) {
+    return (j.row0 + (j.m0 + m) / a.nq) * a.Hq + j.h * a.nq + (j.m0 + m) % a.nq;
+  };
+  if (j.lo >= j.hi) {                            // no keys: this split adds nothing
+    for (int m = threadIdx.x; m < j.m_n; m += (64 * W))
+      a.part_ml[j.split * RH + rowhead(m)] = make_float2(-INFINITY, 0.f);
+    return;
+  }
+  const int m0 = wave * 16 * MT;
+  u32x4_t q[MT][C::QR];
+  pa_queries<C, Tv>(q, a, j, rowhead, m0);
+  f32x4_t o[MT][DT];
+  float m_run[MT], l_run[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    m_run[i] = -INFINITY;
+    l_run[i] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[i][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  // K chunks XORed with the row, so that sixteen rows' reads of one chunk meet
+  // different banks; V as PaCore::stage does
+  auto swz_k = [](int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; };
+  const uint32_t stride = (uint32_t)(a.Hkv * a.D * 2);
+  struct Regs { u32x4_t k[NL], v[NL]; };
+  auto load = [&](Regs& x, int64_t key) {        // keys past hi: zeros
+    const int64_t n = min(max(j.hi - key, (int64_t)1), (int64_t)KEYS);
+    const int64_t from = min(key, j.hi - 1);
+    const int bytes = (int)((uint32_t)(n - 1) * stride + (uint32_t)a.D * 2);
+    const rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(j.k + from * stride), 0, bytes, 0x00027000);
+    const rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(j.v + from * stride), 0, bytes, 0x00027000);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int at = threadIdx.x + i * (64 * W), row = at / CH, c = at % CH;
+      const uint32_t off = c * 8 < a.D && row < KEYS ? (uint32_t)row * stride + c * 16 : kPastEnd;
+      x.k[i] = buf_load16<false>(rk, off, 0);
+      x.v[i] = buf_load16<false>(rv, off, 0);
+    }
+  };
+  auto store = [&](const Regs& x, char* buf) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int at = threadIdx.x + i * (64 * W), row = at / CH, c = at % CH;
+      if (KEYS * CH < 64 * W && row >= KEYS) break;
+      *reinterpret_cast<u32x4_t*>(buf + (row * CH + (c ^ swz_k(row))) * 16) = x.k[i];
+      *reinterpret_cast<u32x4_t*>(buf + kTile + (row * CH + (c ^ C::swz(row))) * 16) = x.v[i];
+    }
+  };
+  auto barrier = []() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  auto step = [&](const char* buf, int64_t key) {
+    f32x4_t s[MT][2];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) s[i][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int t = 0; t < C::QR; ++t) {
+        const int row = 16 * kt + r;
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(
+            buf + (row * CH + ((4 * t + q4) ^ swz_k(row))) * 16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) C::mfma(s[i][kt], k, q[i][t]);
+      }
+    pa_softmax(s, m_run, l_run, o, a.scale2, (int)min(j.hi - key, (int64_t)KEYS));
+    C::template values<MT>(o, s, buf + kTile);
+  };
+  char* const buf0 = lds;
+  char* const buf1 = lds + 2 * kTile;
+  Regs x0, x1;
+  load(x0, j.lo);
+  load(x1, j.lo + KEYS);
+  store(x0, buf0);
+  load(x0, j.lo + 2 * KEYS);
+  barrier();
+  for (int64_t key = j.lo;; key += 2 * KEYS) {
+    store(x1, buf1);
+    load(x1, key + 3 * KEYS);
+    step(buf0, key);
+    barrier();
+    if (key + KEYS >= j.hi) break;
+    store(x0, buf0);
+    load(x0, key + 4 * KEYS);
+    step(buf1, key + KEYS);
+    barrier();
+    if (key + 2 * KEYS >= j.hi) break;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const float l = quad_sum(l_run[i]);
+    const int m = m0 + 16 * i + r;
+    if (m >= j.m_n) continue;
+    const int64_t at = j.split * RH + rowhead(m);
+    if (q4 == 0) a.part_ml[at] = make_float2(m_run[i], l);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int d = 16 * dt + 4 * q4;            // D is a multiple of 8
+      if (d < a.D) *reinterpret_cast<f32x4_t*>(a.part_o + at * a.D + d) = o[i][dt];
+    }
+  }
 }
 
-// Row r, head h: the splits' O, sums and maxima joined. tpr threads (a power of
-// two, at least D / 4) a row and head.
-template <typename Tv>
-__global__ void __launch_bounds__(kPaThreads)
-pa_join_kernel(PaArgs a, int tpr_shift, Tv* __restrict__ out, float* __restrict__ lse) {
-  const int64_t RH = a.R * a.Hq;
-  const int64_t at = ((int64_t)blockIdx.x * kPaThreads + threadIdx.x) >> tpr_shift;
-  const int d = 4 * (threadIdx.x & ((1 << tpr_shift) - 1));
-  if (at >= RH || d >= a.D) return;
-  const int64_t row = at / a.Hq;
-  if (row < group_row(a, 0) || row >= group_row(a, a.G)) return;
-  const int n = a.splits_p + a.splits_s;
-  float m = -INFINITY;
-  for (int p = 0; p < n; ++p) m = fmaxf(m, a.part_ml[p * RH + at].x);
-  const float mu = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < n; ++p) {
-    const float2 ml = a.part_ml[p * RH + at];
-    if (ml.y == 0.f) continue;                   // a split without keys wrote no O
-    const float f = __builtin_amdgcn_exp2f(ml.x - mu);
-    l += ml.y * f;
-    o += *reinterpret_cast<const f32x4_t*>(a.part_o + (p * RH + at) * a.D + d) * f;
+// MT: 16-column tiles of a prefix block (ROWS: of each of its waves); suffix blocks
+// have one. Two waves a SIMD hide each other's waits, so many columns go to eight
+// waves of two tiles (four waves of four tiles, one a SIMD, whose accumulators also
+// travel between the two halves of the register file: 64 rows of four heads behind
+// 65536 keys 283 us).
+constexpr int pa_waves(bool rows) { return rows ? 8 : 4; }
+constexpr int pa_columns(int mt, bool rows) { return 16 * mt * (rows ? pa_waves(true) : 1); }
+constexpr int pa_occupancy(int elt, int mt, int dp, bool rows) {
+  return rows ? 2 : mt == 4 || dp == 256 ? 1 : mt == 1 && elt * dp <= 256 ? 3 : 2;
+}
+
+template <typename Tv, int DP, int MT, bool ROWS>
+__global__ void __launch_bounds__(64 * pa_waves(ROWS), pa_occupancy(sizeof(Tv), MT, DP, ROWS))
+pa_kernel(PaArgs a) {
+  using C = PaCore<Tv, DP>;
+  constexpr int W = pa_waves(ROWS);
+  __shared__ __attribute__((aligned(16))) char lds[W * C::kStage];
+  __shared__ float s_m[W][64], s_l[W][64];
+  static_assert(C::kStage >= C::DT * kWave * 16, "O of the waves");
+  static_assert(!ROWS || W * C::kStage >= 4 * 32 * DP * 2, "two buffers of K and V");
+  PaJob j;
+  if (!find_job<Tv, pa_columns(MT, ROWS)>(a, blockIdx.x, j)) return;
+  if ((int64_t)blockIdx.x >= a.blocks_p) {
+    pa_block<Tv, DP, 1, W>(a, j, lds, s_m, s_l);
+  } else if constexpr (ROWS) {
+    pa_rows_block<DP, MT, W>(a, j, lds);
+  } else {
+    pa_block<Tv, DP, MT, W>(a, j, lds, s_m, s_l);
   }
+}
+
+// Row r, head h: the splits' O, sums and maxima joined. tpr threads (at least
+// D / 4) take four dimensions each, sg groups of them share the splits (both powers
+// of two), so that a thread has few loads in a row: these launches are latency.
+template <typename Tv>
+__global__ void __launch_bounds__(kJoinThreads)
+pa_join_kernel(PaArgs a, int tpr_shift, int sg_shift, Tv* __restrict__ out,
+               float* __restrict__ lse) {
+  __shared__ f32x4_t s_o[kJoinThreads];
+  __shared__ float2 s_ml[kJoinThreads];
+  const int64_t RH = a.R * a.Hq;
+  const int tpr = 1 << tpr_shift, sg = 1 << sg_shift;
+  const int64_t at = (int64_t)blockIdx.x * (kJoinThreads >> (tpr_shift + sg_shift)) +
+                     (threadIdx.x >> (tpr_shift + sg_shift));
+  const int d = 4 * (threadIdx.x & (tpr - 1)), g = (threadIdx.x >> tpr_shift) & (sg - 1);
+  const int64_t row = at / a.Hq;
+  const bool live = at < RH && row >= group_row(a, 0) && row < group_row(a, a.G);
+  const int n = a.splits_p + a.splits_s;
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  if (live && d < a.D) {
+#pragma unroll 4
+    for (int p = g; p < n; p += sg) {
+      const float2 ml = a.part_ml[p * RH + at];
+      const f32x4_t po = *reinterpret_cast<const f32x4_t*>(a.part_o + (p * RH + at) * a.D + d);
+      if (ml.y == 0.f) continue;                 // a split without keys wrote no O
+      const float top = fmaxf(m, ml.x), mu = top == -INFINITY ? 0.f : top;
+      const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
+      l = l * f0 + ml.y * f1;
+      o = o * f0 + po * f1;
+      m = top;
+    }
+  }
+  if (sg > 1) {
+    s_o[threadIdx.x] = o;
+    s_ml[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (g != 0) return;
+    for (int i = 1; i < sg; ++i) {               // in split group order
+      const float2 ml = s_ml[threadIdx.x + (i << tpr_shift)];
+      if (ml.y == 0.f) continue;
+      const float top = fmaxf(m, ml.x), mu = top == -INFINITY ? 0.f : top;
+      const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
+      l = l * f0 + ml.y * f1;
+      o = o * f0 + s_o[threadIdx.x + (i << tpr_shift)] * f1;
+      m = top;
+    }
+  }
+  if (!live || d >= a.D) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  Tv* const dst = out + at * a.D + d;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if constexpr (sizeof(Tv) == 2) dst[e] = f32_to_bf16(o[e] * inv);
-    else dst[e] = o[e] * inv;
+  o *= inv;
+  Tv* const dst = out + at * a.D + d;            // D is a multiple of 8, out on 16 bytes
+  if constexpr (sizeof(Tv) == 2) {
+    const uint32_t lo = (uint32_t)f32_to_bf16(o[0]) | (uint32_t)f32_to_bf16(o[1]) << 16;
+    const uint32_t hi = (uint32_t)f32_to_bf16(o[2]) | (uint32_t)f32_to_bf16(o[3]) << 16;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+  } else {
+    *reinterpret_cast<f32x4_t*>(dst) = o;
   }
   if (lse && d == 0) lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 struct PaPlan {
   int mt, dp, splits_p, splits_s, tiles_s;
+  bool rows;
   int64_t slots_p, blocks_p, blocks_s;
   size_t o, ml, total;
 };
+
+// Column tiles of a key-splitting block: the most that leaves every instance
+// without a spilled register.
+constexpr int pa_max_tiles(int elt, int dp) {
+  return dp == 256 ? 1 : dp == 128 && elt == 4 ? 2 : 4;
+}
 
 PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t P, int64_t S,
                int32_t dtype) {
@@ -460,21 +664,26 @@ PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t
   const int nq = Hq / Hkv;
   pl.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
   const int64_t cols = ceil_div(R, G) * nq;      // of an average group
-  pl.mt = std::min(cols <= 16 ? 1 : cols <= 32 ? 2 : 4,
-                   pa_max_tiles(dtype == MOE_BF16 ? 2 : 4, pl.dp));
-  pl.slots_p = R * nq / (16 * pl.mt) + G;
+  pl.rows = dtype == MOE_BF16 && pl.dp <= 128 && cols > 64;
+  if (pl.rows) pl.mt = cols <= 128 ? 1 : 2;
+  else pl.mt = std::min(cols <= 16 ? 1 : cols <= 32 ? 2 : 4,
+                        pa_max_tiles(dtype == MOE_BF16 ? 2 : 4, pl.dp));
+  const int bm = pa_columns(pl.mt, pl.rows);
+  pl.slots_p = R * nq / bm + G;
   pl.tiles_s = (int)ceil_div(nq, 16);
-  auto splits = [](int64_t blocks, int64_t keys) {
+  auto splits = [](int64_t blocks, int64_t keys, int64_t want) {
     if (keys == 0) return 0;
     const int64_t most = std::min<int64_t>(ceil_div(keys, 128), 64);
-    return (int)std::min(most, std::max<int64_t>(1, ceil_div(512, blocks)));
+    return (int)std::min(most, std::max<int64_t>(1, ceil_div(want, blocks)));
   };
-  // the tiles of even groups; the upper bound counts one more a group
-  const int64_t used = G * ceil_div(cols, 16 * pl.mt);
-  pl.splits_p = splits(used * Hkv, P);
-  pl.splits_s = splits(R * Hkv * pl.tiles_s, S);
-  pl.blocks_p = pl.splits_p ? ceil_div((int64_t)Hkv * pl.splits_p, 8) * 8 * pl.slots_p : 0;
-  pl.blocks_s = R * Hkv * pl.tiles_s * pl.splits_s;
+  // the tiles of even groups (the upper bound counts one more a group); blocks of
+  // many registers are one a compute unit, and a second round of them costs more
+  // than the join of fewer splits saves
+  const int64_t used = G * ceil_div(cols, bm);
+  pl.splits_p = splits(used * Hkv, P, pl.rows && pl.mt == 2 ? 256 : 512);
+  pl.splits_s = splits(R * Hkv * pl.tiles_s, S, 512);
+  pl.blocks_p = ceil_div(pl.slots_p * pl.splits_p, 8) * 8 * Hkv;
+  pl.blocks_s = ceil_div(R * pl.tiles_s * pl.splits_s, 8) * 8 * Hkv;
   const size_t n = (size_t)(pl.splits_p + pl.splits_s) * R * Hq;
   pl.o = 0;
   pl.ml = align_up(n * D * 4, 256);
@@ -499,13 +708,23 @@ bool pa_supported(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int6
 }
 
 template <typename Tv, int DP>
-int pa_launch(const PaArgs& a, int mt, unsigned blocks, hipStream_t st) {
+int pa_launch(const PaArgs& a, const PaPlan& pl, unsigned blocks, hipStream_t st) {
   constexpr int M = pa_max_tiles(sizeof(Tv), DP);
-  if (mt == 1) pa_kernel<Tv, DP, 1><<<dim3(blocks), dim3(kPaThreads), 0, st>>>(a);
+  if constexpr (sizeof(Tv) == 2 && DP <= 128) {
+    if (pl.rows) {
+      constexpr int T = 64 * pa_waves(true);
+      if (pl.mt == 1) pa_kernel<Tv, DP, 1, true><<<dim3(blocks), dim3(T), 0, st>>>(a);
+      else pa_kernel<Tv, DP, 2, true><<<dim3(blocks), dim3(T), 0, st>>>(a);
+      MOE_CHECK_LAUNCH();
+      return MOE_OK;
+    }
+  }
+  constexpr int T = 64 * pa_waves(false);
+  if (pl.mt == 1) pa_kernel<Tv, DP, 1, false><<<dim3(blocks), dim3(T), 0, st>>>(a);
   if constexpr (M >= 2)
-    if (mt == 2) pa_kernel<Tv, DP, 2><<<dim3(blocks), dim3(kPaThreads), 0, st>>>(a);
+    if (pl.mt == 2) pa_kernel<Tv, DP, 2, false><<<dim3(blocks), dim3(T), 0, st>>>(a);
   if constexpr (M >= 4)
-    if (mt == 4) pa_kernel<Tv, DP, 4><<<dim3(blocks), dim3(kPaThreads), 0, st>>>(a);
+    if (pl.mt == 4) pa_kernel<Tv, DP, 4, false><<<dim3(blocks), dim3(T), 0, st>>>(a);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
@@ -515,14 +734,16 @@ int pa_run(const PaArgs& a, const PaPlan& pl, Tv* out, float* lse, hipStream_t s
   const unsigned blocks = (unsigned)(pl.blocks_p + pl.blocks_s);
   int rc = MOE_OK;
   if (blocks) {
-    rc = pl.dp == 64 ? pa_launch<Tv, 64>(a, pl.mt, blocks, st)
-       : pl.dp == 128 ? pa_launch<Tv, 128>(a, pl.mt, blocks, st)
-                      : pa_launch<Tv, 256>(a, pl.mt, blocks, st);
+    rc = pl.dp == 64 ? pa_launch<Tv, 64>(a, pl, blocks, st)
+       : pl.dp == 128 ? pa_launch<Tv, 128>(a, pl, blocks, st)
+                      : pa_launch<Tv, 256>(a, pl, blocks, st);
   }
   if (rc != MOE_OK) return rc;
   const int shift = a.D <= 64 ? 4 : a.D <= 128 ? 5 : 6;
-  const unsigned grid = (unsigned)ceil_div(a.R * a.Hq, kPaThreads >> shift);
-  pa_join_kernel<Tv><<<dim3(grid), dim3(kPaThreads), 0, st>>>(a, shift, out, lse);
+  int sg = 0;                                    // log2 of the split groups
+  while (sg < 8 - shift && (2 << sg) <= pl.splits_p + pl.splits_s) ++sg;
+  const unsigned grid = (unsigned)ceil_div(a.R * a.Hq, kJoinThreads >> (shift + sg));
+  pa_join_kernel<Tv><<<dim3(grid), dim3(kJoinThreads), 0, st>>>(a, shift, sg, out, lse);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
@@ -576,7 +797,11 @@ extern "C" int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int
   a.Hkv = Hkv;
   a.D = D;
   a.nq = Hq / Hkv;
-  a.scale2 = scale * kLog2e;
+  // never 0, which would make a masked key's score NaN: then the queries are zeros
+  const bool none = fabsf(scale) < 1e-37f;
+  a.scale2 = none ? 1.f : std::min(fabsf(scale) * kLog2e, 3e38f);
+  a.keep = none ? 0u : ~0u;
+  a.flip = none || scale >= 0.f ? 0u : dtype == MOE_BF16 ? 0x80008000u : 0x80000000u;
   a.splits_p = pl.splits_p;
   a.splits_s = pl.splits_s;
   a.blocks_p = pl.blocks_p;

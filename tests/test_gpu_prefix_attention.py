@@ -123,6 +123,30 @@ def test_shared_by_many_rows(rows, Hq, Hkv):
     _check(c, "bf16", 0.09, even=True)
 
 
+@pytest.mark.parametrize("rows,P,D", [(33, 1, 128), (17, 63, 64), (40, 64, 128), (70, 65, 40),
+                                      (70, 31, 128), (35, 97, 104), (100, 700, 64)])
+def test_shared_by_more_rows_than_a_block_has(rows, P, D):
+    # more than 64 and more than 128 columns: whole and cut steps, lengths that leave
+    # parts without a key, a group of few rows beside the large one
+    c, g = _case("bf16", [0, rows, rows + 1, rows + 3], rows + 5, 8, 2, D, P, 9, rows + P)
+    c["pl"][0] = P
+    _check(c, "bf16", D ** -0.5)
+    _check(c, "bf16", -0.3)
+    c["pl"][:] = 0
+    _check(c, "bf16", 0.1)
+
+
+@pytest.mark.parametrize("rows", [5, 40])
+def test_scale_of_zero_is_the_mean(rows):
+    # scores of 1e36 times 0: equal weights, masked keys none
+    c, g = _case("bf16", [0, rows, rows + 2], rows + 2, 8, 2, 64, 45, 6, 9)
+    c["pl"][0] = 37
+    for n in ("q", "kp", "ks"):
+        c[n] = synth.bf16_bits((_f(c[n]) * 1e17).astype(np.float32))
+    _check(c, "bf16", 0.0)
+    _check(c, "bf16", -0.0)
+
+
 def test_groups_rows_outside_and_bad_numbers():
     # rows before the first group and behind the last keep their outputs; lengths
     # and offsets outside their range are clipped
