@@ -721,9 +721,10 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
 _CURRENT = contextlib.nullcontext()
 
 
-def _one_device(*ts):
+def _one_device(stream, *ts):
     """Every given tensor contiguous, on one GPU: a context in which that is the
-    current device (its current stream is the one the call goes to)."""
+    current device and `stream`, if there is one, the current stream, so that what
+    the call allocates or fills belongs to the stream that it goes to."""
     dev = -1
     for t in ts:
         if t is None:
@@ -738,6 +739,10 @@ def _one_device(*ts):
         elif d != dev:
             raise ValueError("every tensor must be on the same GPU")
     cuda = _torch().cuda
+    if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError("the stream must be of the tensors' GPU")
+        return cuda.stream(stream)
     return _CURRENT if dev == cuda.current_device() else cuda.device(dev)
 
 
@@ -750,12 +755,10 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _raw_stream(stream=None):
-    """The given stream, else the current one of the current device, as an
-    address (without an object for it)."""
+def _raw_stream():
+    """The current stream of the current device, as an address (without an object
+    for it)."""
     torch = _torch()
-    if stream is not None:
-        return stream.cuda_stream
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
@@ -805,7 +808,7 @@ def prefix_attention(q, k_prefix=None, v_prefix=None, k_suffix=None, v_suffix=No
     _want("group_offsets", group_offsets, (G + 1,), torch.int32)
     _want("out", out, (R, Hq, D), q.dtype)
     _want("lse", lse, (R, Hq), torch.float32)
-    with _one_device(q, k_prefix, v_prefix, k_suffix, v_suffix, prefix_len, suffix_len,
+    with _one_device(stream, q, k_prefix, v_prefix, k_suffix, v_suffix, prefix_len, suffix_len,
                      group_offsets, out, lse, workspace):
         if out is None:                # rows of no group are left as they are
             out = torch.empty_like(q) if group_offsets is None else torch.zeros_like(q)
@@ -817,7 +820,7 @@ def prefix_attention(q, k_prefix=None, v_prefix=None, k_suffix=None, v_suffix=No
             _addr(q), dt, R, Hq, Hkv, D, _addr(group_offsets), G, _addr(k_prefix), _addr(v_prefix), P,
             _addr(prefix_len), _addr(k_suffix), _addr(v_suffix), S, _addr(suffix_len),
             float(D ** -0.5 if scale is None else scale), _addr(out), _addr(lse), _addr(ws), nbytes,
-            _raw_stream(stream))
+            _raw_stream())
     _check("moe_prefix_attention", st)
     return out, lse
 
@@ -864,7 +867,7 @@ def layer_decode(x, w_router, w_gate, w_up, w_down, k, bias=None, renormalize=Tr
     _want("incomplete", incomplete, (T,), torch.int32)
     if accumulate and y is None:
         raise ValueError("accumulate needs an existing y")
-    with _one_device(x, w_router, w_gate, w_up, w_down, bias, slot_of_expert, sg, su, sd, y,
+    with _one_device(stream, x, w_router, w_gate, w_up, w_down, bias, slot_of_expert, sg, su, sd, y,
                      topk_idx, topk_w, incomplete, workspace):
         dev = x.device
         if y is None:
@@ -880,7 +883,7 @@ def layer_decode(x, w_router, w_gate, w_up, w_down, k, bias=None, renormalize=Tr
                                   1 if renormalize else 0, _addr(w_gate), _addr(w_up), _addr(w_down),
                                   S, F, _addr(slot_of_expert), _addr(sg), _addr(su), _addr(sd), Fs,
                                   1 if accumulate else 0, _addr(y), _addr(topk_idx), _addr(topk_w),
-                                  _addr(incomplete), _addr(ws), nbytes, _raw_stream(stream))
+                                  _addr(incomplete), _addr(ws), nbytes, _raw_stream())
     _check("moe_layer_decode", st)
     return y, topk_idx, topk_w, incomplete
 
@@ -911,7 +914,7 @@ def beam_select(logits, scores, n_out=None, finished=None, eos=None, parent=None
     for name, t in (("parent", parent), ("token", token), ("out_finished", out_finished)):
         _want(name, t, (B, n_out), torch.int32)
     _want("out_scores", out_scores, (B, n_out), torch.float32)
-    with _one_device(logits, scores, finished, parent, token, out_scores, out_finished,
+    with _one_device(stream, logits, scores, finished, parent, token, out_scores, out_finished,
                      workspace):
         new = lambda t, dtype: torch.empty((B, n_out), dtype=dtype, device=logits.device) \
             if t is None else t
@@ -924,7 +927,7 @@ def beam_select(logits, scores, n_out=None, finished=None, eos=None, parent=None
         st = lib.moe_beam_select(_addr(logits), dt, B, K, V, _addr(scores), _addr(finished),
                                  -1 if eos is None else int(eos), n_out, _addr(parent), _addr(token),
                                  _addr(out_scores), _addr(out_finished), _addr(ws), nbytes,
-                                 _raw_stream(stream))
+                                 _raw_stream())
     _check("moe_beam_select", st)
     return parent, token, out_scores, out_finished
 
@@ -955,7 +958,7 @@ def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None
     _want("lens", lens, (R,), torch.int32)
     _want("new_lens", new_lens, (R,), torch.int32)
     _want("err", err, (1,), torch.int32)
-    with _one_device(*caches, parent, lens, new_lens, err):
+    with _one_device(stream, *caches, parent, lens, new_lens, err):
         dev = parent.device
         if new_lens is None:
             new_lens = torch.empty(R, dtype=torch.int32, device=dev)
@@ -963,6 +966,6 @@ def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None
             err = torch.zeros(1, dtype=torch.int32, device=dev)
         ptrs = (ctypes.c_void_p * len(caches))(*[c.data_ptr() for c in caches])
         st = lib.moe_beam_reorder(ptrs, len(caches), L, B, K, S, unit, _addr(parent), _addr(lens),
-                                  _addr(new_lens), _addr(err), _raw_stream(stream))
+                                  _addr(new_lens), _addr(err), _raw_stream())
     _check("moe_beam_reorder", st)
     return new_lens, err

@@ -272,3 +272,59 @@ def test_given_stream_is_the_one_that_is_used():
         torch.cuda.synchronize()
         for n, t in s["out"].items():
             assert torch.equal(want[n], t), n
+
+
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Outputs, fills and workspaces of a call on a given stream, while the current
+    stream is far behind and reuses memory at once."""
+    s = _state(5)
+    off = torch.tensor([0, 3, 5], dtype=torch.int32, device=DEV)      # row 5 is in no group
+    shape = (s["q"], s["kp"], s["vp"], s["ks"], s["vs"])
+
+    def calls(stream):
+        a, lse = ops.prefix_attention(*shape, group_offsets=off, stream=stream)
+        y, idx, w, inc = ops.layer_decode(s["x"], s["wr"], s["wg"], s["wu"], s["wd"], 2, stream=stream)
+        p, t, sc, _ = ops.beam_select(s["logits"], s["scores"], 4, stream=stream)
+        n, err = ops.beam_reorder([s["out"]["moved"]], s["parent"], stream=stream)
+        return [a, lse, y, idx, w, inc, p, t, sc, n, err]
+
+    want = [t.clone() for t in calls(None)]
+    assert want[1][5].isinf().all() and int(want[10]) == 0
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn((4096, 4096), device=DEV)
+    for _ in range(3):
+        for _ in range(20):
+            big = big @ big * 1e-4
+        got = calls(side)
+        junk = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for n in (1 << 10, 1 << 14, 1 << 18)]
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g, w)
+        del junk
+
+
+def test_long_offsets_in_a_cache():
+    """Keys that lie beyond 2^32 bytes, of rows whose caches are that far apart."""
+    R, S, D = 3, 1 << 22, 128                                   # 1 GiB a row and cache
+    k = torch.zeros((R, S, 1, D), dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    q = torch.zeros((R, 4, D), dtype=torch.bfloat16, device=DEV)
+    q[:, :, 0] = 1.0
+    at = [S - 1, S - 70, 5]
+    for r in range(R):
+        k[r, at[r], 0, 0] = 60.0
+        v[r, at[r], 0, :] = r + 1.0
+    k[2, S // 2:, 0, 1] = float("nan")                          # behind the row's length
+    lens = torch.tensor([S, S, S // 2], dtype=torch.int32, device=DEV)
+    out, lse = ops.prefix_attention(q, None, None, k, v, suffix_len=lens, scale=1.0)
+    # exp(60) against 2^22 of exp(0): weight 1 - 4e-20
+    for r in range(R):
+        assert torch.equal(out[r].float(), torch.full((4, D), r + 1.0, device=DEV))
+        assert (lse[r] - 60.0).abs().max() < 60 * 2 ** -22
+    last = k[0, S - 1].clone()
+    moved = torch.tensor([[0, 0, 1]], dtype=torch.int32, device=DEV)
+    n, err = ops.beam_reorder([k[None], v[None]], moved)
+    assert int(err) == 0 and n.tolist() == [S, S, S]
+    assert torch.equal(k[1, S - 1], last) and float(k[2, S - 70, 0, 0]) == 60.0
+    assert float(v[1, S - 1, 0, 5]) == 1.0 and float(v[2, S - 70, 0, 5]) == 2.0
