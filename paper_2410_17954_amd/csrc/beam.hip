@@ -1,11 +1,11 @@
 // moe_beam_select and moe_beam_reorder: the choice of a request's best
 // continuations, and the beams' states following it.
 //
-// Selection is one pass over the logits, which bounds it (HBM). c(b, v) =
-// score_b + z_bv - lse_b ranks a row's tokens by their logits alone, so a block
-// takes a chunk of one row into registers once and leaves the n best of it by
-// logit with its share of the row's log-sum-exp; a second launch, one block a
-// request, adds up the shares and merges the lists.
+// Selection is one pass over the logits. c(b, v) = score_b + z_bv - lse_b ranks a
+// row's tokens by their logits alone, so a block takes a chunk of one row into
+// registers once and leaves the n best of it by logit with its share of the row's
+// log-sum-exp; a second launch, one block a request, adds up the shares and merges
+// the lists.
 // Keys are (value, index) pairs, larger value first, lower index among equal
 // values: no two are equal, which bounds how many can lie above a threshold
 // whatever the logits hold.
@@ -55,7 +55,7 @@ SelLayout sel_layout(int64_t B, int32_t K, int64_t V, int32_t n_out) {
 
 template <typename V>
 __device__ __forceinline__ bool ahead(V a, int32_t ai, V b, int32_t bi) {
-  return a > b || (a == b && ai < bi);
+  return (a > b) | ((a == b) & (ai < bi));       // no branch, behind which a load would wait
 }
 
 // 16 bytes from an address that is only element-aligned.
@@ -108,10 +108,12 @@ __device__ __forceinline__ void group_extremes(float v, int g, float& m, float& 
 //      LDS and are ranked by counting.
 // Where a wave holds more than kSelPart of them (equal logits, sorted ones), n
 // rounds over the registers pick the best after the one before instead.
-// What bounds it is instructions, not HBM: 7 a logit (and an exponential, which
-// counts four) and some 400 a wave and chunk, hence long chunks (64 requests of 8
-// beams over 128000 bf16 logits: chunks of 8192 63 us, of 16384 53; blocks that
-// walk over several with the next one's loads in flight 61).
+// 64 requests of 8 beams over 128000 bf16 logits (131 MB) take 39 us, 34 where the
+// last-level cache holds them: the loads and the maxima 19, the sums 2, the
+// candidates 6, the ranks 11. Blocks that start together load together, so what
+// follows the loads is not hidden behind them, and long chunks have less of it (of
+// 8192 logits 63 us, of 16384 54, both before the ranks lost their branches; blocks
+// that walk over several with the next one's loads in flight were slower).
 constexpr int kSelPart = 128;
 
 template <typename Tv, int EPT>

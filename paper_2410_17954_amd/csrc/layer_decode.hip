@@ -3,7 +3,7 @@
 //
 // So few tokens leave the layer bound by reading the weights of the experts
 // they reach once (HBM); the rest is launches and latencies, so there are three
-// of the former and no permuted copies:
+// of the former (a fourth beyond 16 tokens) and no permuted copies:
 //   ld_first_kernel  the router's logits in float64, spread over the chip, and
 //                    beside them the shared experts' gate and up projections
 //   ld_up_kernel     every block decides the routes of all tokens for itself
