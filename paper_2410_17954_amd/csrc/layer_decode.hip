@@ -4,11 +4,11 @@
 // So few tokens leave the layer bound by reading the weights of the experts
 // they reach once (HBM); the rest is launches and latencies, so there are three
 // of the former (a fourth beyond 16 tokens) and no permuted copies:
-//   ld_first_kernel  the router's logits in float64, spread over the chip, and
-//                    beside them the shared experts' gate and up projections
-//   ld_up_kernel     every block decides the routes of all tokens for itself
-//                    (it needs no other block), then the blocks stream gate and
-//                    up rows and write
+//   ld_first_kernel  the router's logits in float64, spread over the chip
+//   ld_up_kernel     blocks that stream the shared experts' gate and up rows; the
+//                    others each decide the routes of all tokens for themselves
+//                    (none needs another block), then stream the active experts'.
+//                    They write
 //                      a[t, :] = gate_t * silu(x_t . Wg^T) * (x_t . Wu^T)
 //   ld_down_kernel   y[t, n] = sum over the experts of t of a . Wd[n, :]: the
 //                    gates are in a, so the sums of all experts of a column
@@ -440,9 +440,8 @@ struct LdUp {
 
   // K blocks of a batch: as many as leave every instance without a spilled
   // register (at 128 a lane with eight waves, 256 with four)
-  static constexpr int unroll(int mt, bool half) {
-    if (TILES == 2 && MTMAX == 4) return half ? 3 : mt <= 2 ? 2 : 1;
-    if (TILES == 2) return half ? 4 : mt == 1 ? 3 : mt == 2 ? 2 : 1;
+  static constexpr int unroll(int mt) {
+    if (TILES == 2) return mt == 1 ? 3 : mt == 2 ? 2 : 1;
     return mt == 1 ? 2 : 1;
   }
 
@@ -476,7 +475,7 @@ struct LdUp {
 #pragma unroll
       for (int g = 0; g < TILES; ++g) acc[i][g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     struct Block { u32x4_t w[TILES][2]; X x; };
-    ld_stream<unroll(MT, HALF), (MTMAX > 1), Block>(
+    ld_stream<unroll(MT), (MTMAX > 1), Block>(
         nb * wave / W, nb * (wave + 1) / W,
         [&](Block& k, int b) {
           const uint32_t at = (uint32_t)b * 128;
@@ -552,59 +551,68 @@ __device__ __forceinline__ rsrc_t ld_x(const LdArgs& a) {
                                            (int)(a.T * (uint32_t)(a.H * sizeof(Tv))), 0x00027000);
 }
 
-// The logits (a block: one expert, a token a wave) and, in the blocks behind
-// them, the shared experts' gate and up projections, which need no route.
-template <typename Tv, int MTMAX, int NT, int W>
-__global__ void __launch_bounds__(64 * W, W / 2)
-ld_first_kernel(LdArgs a, int logit_blocks) {
-  using Up = LdUp<Tv, MTMAX, NT, W>;
-  __shared__ typename Up::Part part;
-  if ((int)blockIdx.x < logit_blocks) {
-    const int t = blockIdx.x / a.E * W + threadIdx.x / kWave;
-    if (t < a.T)
-      ld_logit(static_cast<const Tv*>(a.x), static_cast<const Tv*>(a.w_router), t,
-               (int)(blockIdx.x % a.E), a.H, a.E, a.bias, a.bias_mode, a.z);
-    return;
-  }
-  Tv* const act = static_cast<Tv*>(a.act) + (int64_t)a.T * a.k * a.F;
-  const int units = (int)((a.Fs + Up::COLS - 1) / Up::COLS), step = gridDim.x - logit_blocks;
-  for (int unit = blockIdx.x - logit_blocks; unit < units; unit += step)
-    Up::run(ld_x<Tv>(a), part, a.T, nullptr, nullptr, static_cast<const Tv*>(a.sh_gate),
-            static_cast<const Tv*>(a.sh_up), a.H, (int64_t)unit * Up::COLS, a.Fs, act);
+// The logits: a block one expert, a token a wave.
+constexpr int kLogitWaves = 4;
+
+template <typename Tv>
+__global__ void __launch_bounds__(64 * kLogitWaves)
+ld_first_kernel(LdArgs a) {
+  const int t = blockIdx.x / a.E * kLogitWaves + threadIdx.x / kWave;
+  if (t < a.T)
+    ld_logit(static_cast<const Tv*>(a.x), static_cast<const Tv*>(a.w_router), t,
+             (int)(blockIdx.x % a.E), a.H, a.E, a.bias, a.bias_mode, a.z);
 }
 
-// The routes, then the units of the active experts.
+// What the call returns of the routes and the launch after reads, by the whole block.
+template <int TOK>
+__device__ __forceinline__ void ld_write_routes(const LdArgs& a, const LdRoutes<TOK>& rt) {
+  const int threads = blockDim.x;
+  for (int q = threadIdx.x; q < a.T * a.k; q += threads) {
+    a.topk_idx[q] = rt.sel[q];
+    a.topk_w[q] = rt.gate[q];
+    a.row_token[q] = rt.row_token[q];
+  }
+  for (int t = threadIdx.x; a.incomplete && t < a.T; t += threads) {
+    int miss = 0;
+    for (int j = 0; j < a.k; ++j) {
+      const int e = rt.sel[t * a.k + j];
+      miss |= e >= 0 && !((rt.mask[e] >> t) & 1);
+    }
+    a.incomplete[t] = miss;
+  }
+  for (int q = threadIdx.x; q < rt.n_active; q += threads) {
+    const int e = rt.list[q];
+    a.entries[q] = LdEntry{rt.slot[e], rt.base[e], (int)__popcll(rt.mask[e])};
+  }
+  if (threadIdx.x == 0) *a.n_entries = rt.n_active;
+}
+
+// The first blocks stream the shared experts' units, which need no route, while the
+// others decide the routes and then stream the units of the active experts (logits,
+// gate and up of a Qwen-shaped token 23.4 us, with the shared units beside the
+// logits 30; of 64 75, 91).
 template <typename Tv, int MTMAX, int NT, int W>
 __global__ void __launch_bounds__(64 * W, W / 2)
-ld_up_kernel(LdArgs a) {
+ld_up_kernel(LdArgs a, int shared_blocks) {
   using Up = LdUp<Tv, MTMAX, NT, W>;
   constexpr int THREADS = 64 * W;
   __shared__ LdRoutes<16 * MTMAX> rt;
   __shared__ typename Up::Part part;
-  ld_routes<16 * MTMAX, THREADS>(a.z, a.T, a.E, a.k, a.renorm, a.slot, a.S, rt);
-  if (blockIdx.x == 0) {
-    for (int q = threadIdx.x; q < a.T * a.k; q += THREADS) {
-      a.topk_idx[q] = rt.sel[q];
-      a.topk_w[q] = rt.gate[q];
-      a.row_token[q] = rt.row_token[q];
-    }
-    for (int t = threadIdx.x; a.incomplete && t < a.T; t += THREADS) {
-      int miss = 0;
-      for (int j = 0; j < a.k; ++j) {
-        const int e = rt.sel[t * a.k + j];
-        miss |= e >= 0 && !((rt.mask[e] >> t) & 1);
-      }
-      a.incomplete[t] = miss;
-    }
-    for (int q = threadIdx.x; q < rt.n_active; q += THREADS) {
-      const int e = rt.list[q];
-      a.entries[q] = LdEntry{rt.slot[e], rt.base[e], (int)__popcll(rt.mask[e])};
-    }
-    if (threadIdx.x == 0) *a.n_entries = rt.n_active;
+  const int sb = blockIdx.x, rb = sb - shared_blocks;
+  if (rb < 0) {
+    Tv* const act = static_cast<Tv*>(a.act) + (int64_t)a.T * a.k * a.F;
+    const int units = (int)((a.Fs + Up::COLS - 1) / Up::COLS);
+    for (int unit = sb; unit < units; unit += shared_blocks)
+      Up::run(ld_x<Tv>(a), part, a.T, nullptr, nullptr, static_cast<const Tv*>(a.sh_gate),
+              static_cast<const Tv*>(a.sh_up), a.H, (int64_t)unit * Up::COLS, a.Fs, act);
+    return;
   }
+  ld_routes<16 * MTMAX, THREADS>(a.z, a.T, a.E, a.k, a.renorm, a.slot, a.S, rt);
+  if (rb == 0) ld_write_routes(a, rt);
   const int ncb = (int)((a.F + Up::COLS - 1) / Up::COLS);
   const int units = __builtin_amdgcn_readfirstlane(rt.n_active) * ncb;
-  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+  const int step = gridDim.x - shared_blocks;
+  for (int unit = rb; unit < units; unit += step) {
     const int e = __builtin_amdgcn_readfirstlane(rt.list[unit / ncb]);
     const int base = __builtin_amdgcn_readfirstlane(rt.base[e]);
     const int m = __builtin_amdgcn_readfirstlane(__popcll(rt.mask[e]));
@@ -807,20 +815,11 @@ int64_t ld_experts(const LdArgs& a) {
 }
 
 template <typename Tv, int MTMAX, int NT, int W>
-int ld_first(const LdArgs& a, hipStream_t st) {
-  const int64_t logits = a.E * ceil_div(a.T, W);
-  const int64_t shared = std::min<int64_t>(ceil_div(a.Fs, 16 * NT), 2 * device_cu_count());
-  ld_first_kernel<Tv, MTMAX, NT, W>
-      <<<dim3((unsigned)(logits + shared)), dim3(64 * W), 0, st>>>(a, (int)logits);
-  MOE_CHECK_LAUNCH();
-  return MOE_OK;
-}
-
-template <typename Tv, int MTMAX, int NT, int W>
 int ld_up(const LdArgs& a, hipStream_t st) {
-  const int64_t units = ld_experts(a) * ceil_div(a.F, 16 * NT);
-  const unsigned grid = (unsigned)std::min<int64_t>(units, 2 * device_cu_count());
-  ld_up_kernel<Tv, MTMAX, NT, W><<<dim3(grid), dim3(64 * W), 0, st>>>(a);
+  const int64_t units = ld_experts(a) * ceil_div(a.F, 16 * NT), most = 2 * device_cu_count();
+  const int shared = (int)std::min<int64_t>(ceil_div(a.Fs, 16 * NT), most);
+  const unsigned grid = (unsigned)(shared + std::min<int64_t>(units, most));
+  ld_up_kernel<Tv, MTMAX, NT, W><<<dim3(grid), dim3(64 * W), 0, st>>>(a, shared);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
@@ -832,9 +831,10 @@ int ld_launch(const LdArgs& a, int accumulate, Tv* y, hipStream_t st) {
   // DeepSeek-shaped 44, 53), else of 16 columns and eight waves, which have all of
   // K in flight (the four experts of a Qwen-shaped token 16.4 us, by wide units 18.0)
   const int64_t cus = device_cu_count(), experts = ld_experts(a);
-  int rc = ceil_div(a.Fs, 32) >= 2 * cus ? ld_first<Tv, MTMAX, 2, 4>(a, st)
-                                         : ld_first<Tv, MTMAX, 1, 8>(a, st);
-  if (rc != MOE_OK) return rc;
+  ld_first_kernel<Tv><<<dim3((unsigned)(a.E * ceil_div(a.T, kLogitWaves))),
+                        dim3(64 * kLogitWaves), 0, st>>>(a);
+  MOE_CHECK_LAUNCH();
+  int rc;
   if constexpr (MTMAX == 4) {                    // four row tiles need the registers of wide units
     rc = ld_up<Tv, MTMAX, 2, 4>(a, st);
   } else {
