@@ -295,12 +295,12 @@ __device__ __forceinline__ void pa_softmax(f32x4_t (&s)[MT][KT], float (&m)[MT],
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx[i] = fmaxf(mx[i], s[i][kt][e]);
-    mx[i] = quad_max(mx[i]) * scale2;
-    raise = raise || mx[i] > m[i] + kSlack;
+    raise = raise | (mx[i] * scale2 > m[i] + kSlack);
   }
   if (ballot(raise)) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
+      mx[i] = quad_max(mx[i]) * scale2;
       const float to = mx[i] > m[i] + kSlack ? mx[i] : m[i];
       const float f = to == m[i] ? 1.f : __builtin_amdgcn_exp2f(m[i] - to);   // 0 from -inf
       m[i] = to;
