@@ -327,12 +327,12 @@ __device__ __forceinline__ void merge_ranks(const double* key, const int32_t* po
 // a block is bound by its loads' latency: the lists go to LDS beside the rows'
 // sums where they fit.
 __global__ void __launch_bounds__(kMergeThreads)
-beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* __restrict__ scores,
-                  const int32_t* __restrict__ finished, int64_t eos,
+beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
+                  const int32_t* finished, int64_t eos,
                   const double2* __restrict__ stat, const float* __restrict__ val,
                   const int32_t* __restrict__ idx, int32_t* __restrict__ parent,
-                  int32_t* __restrict__ token, float* __restrict__ out_scores,
-                  int32_t* __restrict__ out_finished) {
+                  int32_t* __restrict__ token, float* out_scores,
+                  int32_t* out_finished) {
   __shared__ double s_key[kMergeLists];          // first keys, then the keys to rank
   __shared__ int32_t s_pos[kMergeLists];         // beam << 25 | token: in the order of both
   __shared__ int32_t s_rank[kMergeLists];
@@ -620,6 +620,8 @@ extern "C" int moe_beam_select(const void* logits, int32_t dtype, int64_t B, int
   const size_t elt = dtype == MOE_BF16 ? 2 : 4;
   MOE_CHECK_ARG(reinterpret_cast<uintptr_t>(logits) % elt == 0);
   if (!sel_supported(B, K, V, n_out)) return MOE_ERR_UNSUPPORTED;
+  // in place a block would overwrite what another has yet to read
+  MOE_CHECK_ARG(n_out == K || (out_scores != scores && (!finished || out_finished != finished)));
   const SelLayout lay = sel_layout(B, K, V, n_out);
   if (!workspace || ws_bytes < lay.total || (reinterpret_cast<uintptr_t>(workspace) & 255))
     return MOE_ERR_WORKSPACE;

@@ -193,3 +193,15 @@ def test_oracle_attention_closed_forms():
     # no key at all
     a = oracle.prefix_attention(q[:1], kp, vp, [0], ks, vs, [0], [0, 1], 0.7)
     assert not a[0].any() and (a[1] == -np.inf).all()
+
+
+def test_beam_select_in_place_only_where_rows_keep_their_places(lib):
+    def call(n=4, best=ctypes.c_void_p(0x2000), flags=ctypes.c_void_p(0x3000)):
+        return lib.moe_beam_select(FAKE, 1, 2, 4, 100, FAKE, FAKE, 0, n, FAKE, FAKE, best, flags,
+                                   None, BIG, None)
+
+    for same in (dict(), dict(best=FAKE), dict(flags=FAKE)):
+        assert call(**same) == ops.MOE_ERR_WORKSPACE  # everything but the workspace is right
+    assert call(n=5) == ops.MOE_ERR_WORKSPACE
+    assert call(n=5, best=FAKE) == ops.MOE_ERR_ARG
+    assert call(n=3, flags=FAKE) == ops.MOE_ERR_ARG

@@ -328,3 +328,62 @@ def test_long_offsets_in_a_cache():
     assert int(err) == 0 and n.tolist() == [S, S, S]
     assert torch.equal(k[1, S - 1], last) and float(k[2, S - 70, 0, 0]) == 60.0
     assert float(v[1, S - 1, 0, 5]) == 1.0 and float(v[2, S - 70, 0, 5]) == 2.0
+
+
+@pytest.mark.parametrize("K,V,n", [(1, 1 << 25, 64), (32, 1 << 20, 64)])
+def test_select_at_its_limit(K, V, n):
+    g = torch.Generator(device=DEV).manual_seed(K)
+    z = torch.randn((1, K, V), device=DEV, generator=g).bfloat16()
+    s = torch.randn((1, K), device=DEV, generator=g)
+    parent, token, score, _ = ops.beam_select(z, s, n)
+    c = z.double()
+    c += (s.double() - torch.logsumexp(c, -1))[..., None]
+    c = c.view(-1)
+    # bfloat16 logits tie: in the order of value, then beam and token
+    least = torch.topk(c, n).values[-1]
+    at = torch.nonzero(c >= least).view(-1)
+    order = torch.sort(c[at], descending=True, stable=True).indices[:n]
+    at = at[order]
+    assert torch.equal(parent[0].long(), at // V) and torch.equal(token[0].long(), at % V)
+    # log V + 18 steps of float32 for the sum, one for the result
+    assert ((score[0] - c[at]).abs() <= 2.0 ** -24 * c[at].abs() + 40 * 2.0 ** -23).all()
+
+
+@pytest.mark.parametrize("L,B,K", [(1, 9001, 2), (4100, 1, 3)])
+def test_reorder_more_requests_and_layers_than_a_grid_has(L, B, K):
+    g = torch.Generator(device=DEV).manual_seed(B)
+    caches = [torch.randint(0, 1 << 30, (L, B * K, 2, 3), device=DEV, dtype=torch.int32, generator=g)
+              for _ in range(2)]
+    parent = torch.randint(0, K, (B, K), device=DEV, dtype=torch.int32, generator=g)
+    parent += K * torch.arange(B, device=DEV, dtype=torch.int32)[:, None]
+    want = [c[:, parent.view(-1).long()] for c in caches]
+    _, err = ops.beam_reorder(caches, parent)
+    assert int(err) == 0
+    for c, w in zip(caches, want):
+        assert torch.equal(c, w)
+
+
+def test_attention_of_many_rows():
+    # groups of one row: more blocks than a grid dimension of 65535 would take
+    R, P, D = 70001, 3, 8
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q, k, v = (torch.randn(s, device=DEV, generator=g) for s in ((R, 2, D), (R, P, 1, D), (R, P, 1, D)))
+    out, lse = ops.prefix_attention(q, k, v, scale=1.0)
+    s = (q.double()[:, :, None] * k.double().transpose(1, 2)).sum(-1)     # [R, 2, P]
+    want = (torch.softmax(s, -1)[..., None] * v.double().transpose(1, 2)).sum(2)
+    # scores err by 8 terms x 2^-24 of up to 40, which weigh as such in the result
+    assert (out - want).abs().max() < 40 * 8 * 2.0 ** -24 * 2 * 5
+    assert (lse - torch.logsumexp(s, -1)).abs().max() < 40 * 8 * 2.0 ** -24 * 2
+
+
+def test_select_in_place():
+    g = torch.Generator(device=DEV).manual_seed(8)
+    B, K, V = 50, 4, 3001
+    z = torch.randn((B, K, V), device=DEV, generator=g)
+    s = torch.randn((B, K), device=DEV, generator=g)
+    f = (torch.rand((B, K), device=DEV, generator=g) < 0.3).int()
+    want = ops.beam_select(z, s, finished=f, eos=5)
+    got = ops.beam_select(z, s, finished=f, eos=5, out_scores=s, out_finished=f)
+    assert got[2] is s and got[3] is f
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
