@@ -16,7 +16,8 @@
 // Waves of a block take 32 keys (16 in float32) at a time in turn and keep a
 // maximum, sum and O of their own, so there is no barrier in the loop; they are
 // added up through LDS at the end. Long key ranges are split over blocks, and a
-// second launch joins the splits of prefix and suffix.
+// second launch joins the splits of prefix and suffix; where keys and rows are few, a
+// block does a row's prefix and suffix in one launch.
 #include "moeflow_decode.h"
 #include "common.h"
 #include "buffers.h"
@@ -46,6 +47,8 @@ struct PaArgs {
   int tiles_s;                                   // row tiles of a suffix
   float* part_o;                                 // [splits_p + splits_s][R * Hq][D]
   float2* part_ml;                               // [splits_p + splits_s][R * Hq]: max (log2), sum
+  void* out;
+  float* lse;
 };
 
 __device__ __forceinline__ int64_t group_row(const PaArgs& a, int64_t g) {
@@ -54,12 +57,20 @@ __device__ __forceinline__ int64_t group_row(const PaArgs& a, int64_t g) {
 }
 
 // What a block works on: `m_n` query columns from m0 on (column m is row
-// row0 + m / nq, query head h * nq + m % nq), keys [lo, hi) of a cache.
+// row0 + m / nq, query head h * nq + m % nq), keys [lo, hi) of a cache and, of a
+// whole row, [0, hi2) of another.
 struct PaJob {
-  const char *k, *v;                             // of key 0, head h
-  int64_t lo, hi, row0;
+  const char *k, *v, *k2, *v2;                   // of key 0, head h
+  int64_t lo, hi, hi2, row0;
   int m0, m_n, h, split;
 };
+
+__device__ __forceinline__ int64_t pa_prefix_len(const PaArgs& a, int64_t g) {
+  return a.prefix_len ? min(max((int64_t)a.prefix_len[g], (int64_t)0), a.P) : a.P;
+}
+__device__ __forceinline__ int64_t pa_suffix_len(const PaArgs& a, int64_t r) {
+  return a.suffix_len ? min(max((int64_t)a.suffix_len[r], (int64_t)0), a.S) : a.S;
+}
 
 // Row tiles of group g start at slot floor(first row * nq / BM) + g: slots of
 // different groups never meet, and a slot's group is found without a scan.
@@ -94,7 +105,7 @@ __device__ __forceinline__ bool find_job(const PaArgs& a, int64_t block, PaJob& 
     const int64_t at = (lo * a.P * a.Hkv + j.h) * a.D;
     j.k = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k_prefix) + at);
     j.v = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v_prefix) + at);
-    len = a.prefix_len ? min(max((int64_t)a.prefix_len[lo], (int64_t)0), a.P) : a.P;
+    len = pa_prefix_len(a, lo);
     const int64_t per = ((len + a.splits_p - 1) / a.splits_p + 31) / 32 * 32;
     j.lo = min(len, per * j.split);
     j.hi = min(len, j.lo + per);
@@ -109,11 +120,36 @@ __device__ __forceinline__ bool find_job(const PaArgs& a, int64_t block, PaJob& 
   const int64_t at = (j.row0 * a.S * a.Hkv + j.h) * a.D;
   j.k = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k_suffix) + at);
   j.v = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v_suffix) + at);
-  len = a.suffix_len ? min(max((int64_t)a.suffix_len[j.row0], (int64_t)0), a.S) : a.S;
+  len = pa_suffix_len(a, j.row0);
   const int64_t per = ((len + a.splits_s - 1) / a.splits_s + 31) / 32 * 32;
   j.lo = min(len, per * j.split);
   j.hi = min(len, j.lo + per);
   j.split += a.splits_p;
+  return true;
+}
+
+// Block -> row, key head and column tile of a call that needs no splits.
+template <typename Tv>
+__device__ __forceinline__ bool find_row(const PaArgs& a, int64_t block, PaJob& j) {
+  j.h = (int)(block % a.Hkv);
+  j.m0 = (int)(block / a.Hkv % a.tiles_s) * 16;
+  j.m_n = min(a.nq - j.m0, 16);
+  j.row0 = block / a.Hkv / a.tiles_s;
+  int64_t g = 0, end = a.G;                      // last group that starts at or before the row
+  while (end - g > 1) {
+    const int64_t mid = (g + end) / 2;
+    if (group_row(a, mid) <= j.row0) g = mid;
+    else end = mid;
+  }
+  if (j.row0 < group_row(a, g) || j.row0 >= group_row(a, g + 1)) return false;
+  const int64_t p = (g * a.P * a.Hkv + j.h) * a.D, s = (j.row0 * a.S * a.Hkv + j.h) * a.D;
+  j.k = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k_prefix) + p);
+  j.v = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v_prefix) + p);
+  j.k2 = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k_suffix) + s);
+  j.v2 = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v_suffix) + s);
+  j.lo = 0;
+  j.hi = pa_prefix_len(a, g);
+  j.hi2 = pa_suffix_len(a, j.row0);
   return true;
 }
 
@@ -345,7 +381,19 @@ __device__ __forceinline__ void pa_queries(u32x4_t (&q)[MT][C::QR], const PaArgs
   }
 }
 
-template <typename Tv, int DP, int MT, int W>
+// Four values of a row's result, D a multiple of 8 and the row on 16 bytes.
+__device__ __forceinline__ void pa_put(uint16_t* dst, f32x4_t o) {
+  const uint32_t lo = (uint32_t)f32_to_bf16(o[0]) | (uint32_t)f32_to_bf16(o[1]) << 16;
+  const uint32_t hi = (uint32_t)f32_to_bf16(o[2]) | (uint32_t)f32_to_bf16(o[3]) << 16;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+}
+__device__ __forceinline__ void pa_put(float* dst, f32x4_t o) { *reinterpret_cast<f32x4_t*>(dst) = o; }
+__device__ __forceinline__ float pa_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// WHOLE: the job is a row's whole work, and the block writes the result.
+template <typename Tv, int DP, int MT, int W, bool WHOLE = false>
 __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* lds,
                                          float (*s_m)[64], float (*s_l)[64]) {
   using C = PaCore<Tv, DP>;
@@ -356,7 +404,7 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
   auto rowhead = [&](int m) {
     return (j.row0 + (j.m0 + m) / a.nq) * a.Hq + j.h * a.nq + (j.m0 + m) % a.nq;
   };
-  if (j.lo >= j.hi) {                            // no keys: this split adds nothing
+  if (!WHOLE && j.lo >= j.hi) {                  // no keys: this split adds nothing
     for (int m = threadIdx.x; m < j.m_n; m += (64 * W))
       a.part_ml[j.split * RH + rowhead(m)] = make_float2(-INFINITY, 0.f);
     return;
@@ -375,25 +423,27 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
   char* const mine = lds + wave * C::kStage;
   const uint32_t stride = (uint32_t)(a.Hkv * a.D * (int)sizeof(Tv));
   typename C::Rows k, v;
-  int64_t key = j.lo + wave * C::KEYS;
-  if (key < j.hi) {
-    C::load(k, j.k, key, j.hi, stride, a.D);
-    C::load(v, j.v, key, j.hi, stride, a.D);
-  }
-  while (key < j.hi) {
+  // steps of the first range, then those of the second
+  const int64_t first = j.hi > j.lo ? (j.hi - j.lo + C::KEYS - 1) / C::KEYS : 0;
+  const int64_t steps = WHOLE ? first + (j.hi2 + C::KEYS - 1) / C::KEYS : first;
+  auto load = [&](int64_t st) {
+    const bool two = WHOLE && st >= first;
+    const int64_t key = two ? (st - first) * C::KEYS : j.lo + st * C::KEYS;
+    C::load(k, two ? j.k2 : j.k, key, two ? j.hi2 : j.hi, stride, a.D);
+    C::load(v, two ? j.v2 : j.v, key, two ? j.hi2 : j.hi, stride, a.D);
+  };
+  if (wave < steps) load(wave);
+  for (int64_t st = wave; st < steps; st += W) {
     f32x4_t s[MT][KT];
     C::template scores<MT>(s, q, k);
     C::stage(mine, v);
-    const int64_t next = key + W * C::KEYS;
-    if (next < j.hi) {
-      C::load(k, j.k, next, j.hi, stride, a.D);
-      C::load(v, j.v, next, j.hi, stride, a.D);
-    }
-    pa_softmax(s, m_run, l_run, o, a.scale2, (int)min(j.hi - key, (int64_t)C::KEYS));
+    if (st + W < steps) load(st + W);
+    const int64_t left = WHOLE && st >= first ? j.hi2 - (st - first) * C::KEYS
+                                              : j.hi - j.lo - st * C::KEYS;
+    pa_softmax(s, m_run, l_run, o, a.scale2, (int)min(left, (int64_t)C::KEYS));
     lds_fence();
     C::template values<MT>(o, s, mine);
     lds_fence();
-    key = next;
   }
   // join the waves: common maximum, then O through LDS, one row tile at a time
 #pragma unroll
@@ -421,14 +471,19 @@ __device__ __forceinline__ void pa_block(const PaArgs& a, const PaJob& j, char* 
     for (int dt = 0; dt < DT; ++dt) part[(wave * DT + dt) * kWave + lane] = o[i][dt] * f;
     __syncthreads();
     if (m < j.m_n) {
-      const int64_t at = j.split * RH + rowhead(m);
-      if (wave == 0 && q4 == 0) a.part_ml[at] = make_float2(top, l);
+      const int64_t at = WHOLE ? rowhead(m) : j.split * RH + rowhead(m);
+      if (wave == 0 && q4 == 0) {
+        if (!WHOLE) a.part_ml[at] = make_float2(top, l);
+        else if (a.lse) a.lse[at] = pa_lse(top, l);
+      }
       for (int dt = wave; dt < DT; dt += W) {
         f32x4_t sum = part[dt * kWave + lane];
 #pragma unroll
         for (int w = 1; w < W; ++w) sum += part[(w * DT + dt) * kWave + lane];
         const int d = 16 * dt + 4 * q4;          // D is a multiple of 8
-        if (d < a.D) *reinterpret_cast<f32x4_t*>(a.part_o + at * a.D + d) = sum;
+        if (d >= a.D) continue;
+        if constexpr (WHOLE) pa_put(static_cast<Tv*>(a.out) + at * a.D + d, sum * (l == 0.f ? 0.f : 1.f / l));
+        else *reinterpret_cast<f32x4_t*>(a.part_o + at * a.D + d) = sum;
       }
     }
     __syncthreads();                             // part is rewritten next
@@ -585,13 +640,29 @@ pa_kernel(PaArgs a) {
   }
 }
 
+// A row and key head a block, prefix and suffix in one go, the result written: one
+// launch where the keys are few.
+constexpr int pa_row_waves(int dp) { return dp == 256 ? 4 : 8; }
+
+template <typename Tv, int DP>
+__global__ void __launch_bounds__(64 * pa_row_waves(DP))
+pa_row_kernel(PaArgs a) {
+  using C = PaCore<Tv, DP>;
+  constexpr int W = pa_row_waves(DP);
+  __shared__ __attribute__((aligned(16))) char lds[W * C::kStage];
+  __shared__ float s_m[W][64], s_l[W][64];
+  static_assert(C::kStage >= C::DT * kWave * 16, "O of the waves");
+  PaJob j;
+  if (!find_row<Tv>(a, blockIdx.x, j)) return;
+  pa_block<Tv, DP, 1, W, true>(a, j, lds, s_m, s_l);
+}
+
 // Row r, head h: the splits' O, sums and maxima joined. tpr threads (at least
 // D / 4) take four dimensions each, sg groups of them share the splits (both powers
 // of two), so that a thread has few loads in a row: these launches are latency.
 template <typename Tv>
 __global__ void __launch_bounds__(kJoinThreads)
-pa_join_kernel(PaArgs a, int tpr_shift, int sg_shift, Tv* __restrict__ out,
-               float* __restrict__ lse) {
+pa_join_kernel(PaArgs a, int tpr_shift, int sg_shift) {
   __shared__ f32x4_t s_o[kJoinThreads];
   __shared__ float2 s_ml[kJoinThreads];
   const int64_t RH = a.R * a.Hq;
@@ -635,20 +706,13 @@ pa_join_kernel(PaArgs a, int tpr_shift, int sg_shift, Tv* __restrict__ out,
   if (!live || d >= a.D) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   o *= inv;
-  Tv* const dst = out + at * a.D + d;            // D is a multiple of 8, out on 16 bytes
-  if constexpr (sizeof(Tv) == 2) {
-    const uint32_t lo = (uint32_t)f32_to_bf16(o[0]) | (uint32_t)f32_to_bf16(o[1]) << 16;
-    const uint32_t hi = (uint32_t)f32_to_bf16(o[2]) | (uint32_t)f32_to_bf16(o[3]) << 16;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
-  } else {
-    *reinterpret_cast<f32x4_t*>(dst) = o;
-  }
-  if (lse && d == 0) lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  pa_put(static_cast<Tv*>(a.out) + at * a.D + d, o);
+  if (a.lse && d == 0) a.lse[at] = pa_lse(m, l);
 }
 
 struct PaPlan {
   int mt, dp, splits_p, splits_s, tiles_s;
-  bool rows;
+  bool rows, whole;                              // whole: a launch of rows, no splits
   int64_t slots_p, blocks_p, blocks_s;
   size_t o, ml, total;
 };
@@ -685,6 +749,13 @@ PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t
   pl.splits_s = splits(R * Hkv * pl.tiles_s, S, 512);
   pl.blocks_p = ceil_div(pl.slots_p * pl.splits_p, 8) * 8 * Hkv;
   pl.blocks_s = ceil_div(R * pl.tiles_s * pl.splits_s, 8) * 8 * Hkv;
+  // a step's loads take some 2.5 us, which two of a wave may cost against a launch and
+  // the join; and while the blocks run at once, loads of a shared prefix by each of its
+  // rows meet in the caches (4 rows behind 250 keys 9.4 us, split 6.8 + 4.2, behind 777
+  // 16.6, 7.2 + 4.5; 64 rows of eight key heads 17.3, 16.3 + 4.1; 256 rows 63, 45 + 6.6)
+  const int64_t keys = dtype == MOE_BF16 ? 32 : 16;
+  pl.whole = R * Hkv * pl.tiles_s <= 512 &&
+             ceil_div(P, keys) + ceil_div(S, keys) <= 2 * pa_row_waves(pl.dp);
   const size_t n = (size_t)(pl.splits_p + pl.splits_s) * R * Hq;
   pl.o = 0;
   pl.ml = align_up(n * D * 4, 256);
@@ -731,7 +802,15 @@ int pa_launch(const PaArgs& a, const PaPlan& pl, unsigned blocks, hipStream_t st
 }
 
 template <typename Tv>
-int pa_run(const PaArgs& a, const PaPlan& pl, Tv* out, float* lse, hipStream_t st) {
+int pa_run(const PaArgs& a, const PaPlan& pl, hipStream_t st) {
+  if (pl.whole) {
+    const dim3 grid((unsigned)(a.R * a.Hkv * a.tiles_s));
+    if (pl.dp == 64) pa_row_kernel<Tv, 64><<<grid, dim3(64 * pa_row_waves(64)), 0, st>>>(a);
+    else if (pl.dp == 128) pa_row_kernel<Tv, 128><<<grid, dim3(64 * pa_row_waves(128)), 0, st>>>(a);
+    else pa_row_kernel<Tv, 256><<<grid, dim3(64 * pa_row_waves(256)), 0, st>>>(a);
+    MOE_CHECK_LAUNCH();
+    return MOE_OK;
+  }
   const unsigned blocks = (unsigned)(pl.blocks_p + pl.blocks_s);
   int rc = MOE_OK;
   if (blocks) {
@@ -744,7 +823,7 @@ int pa_run(const PaArgs& a, const PaPlan& pl, Tv* out, float* lse, hipStream_t s
   int sg = 0;                                    // log2 of the split groups
   while (sg < 8 - shift && (2 << sg) <= pl.splits_p + pl.splits_s) ++sg;
   const unsigned grid = (unsigned)ceil_div(a.R * a.Hq, kJoinThreads >> (shift + sg));
-  pa_join_kernel<Tv><<<dim3(grid), dim3(kJoinThreads), 0, st>>>(a, shift, sg, out, lse);
+  pa_join_kernel<Tv><<<dim3(grid), dim3(kJoinThreads), 0, st>>>(a, shift, sg);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
@@ -810,7 +889,8 @@ extern "C" int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int
   a.tiles_s = pl.tiles_s;
   a.part_o = reinterpret_cast<float*>(ws + pl.o);
   a.part_ml = reinterpret_cast<float2*>(ws + pl.ml);
+  a.out = out;
+  a.lse = lse;
   hipStream_t st = as_stream(stream);
-  return dtype == MOE_BF16 ? pa_run<uint16_t>(a, pl, static_cast<uint16_t*>(out), lse, st)
-                           : pa_run<float>(a, pl, static_cast<float*>(out), lse, st);
+  return dtype == MOE_BF16 ? pa_run<uint16_t>(a, pl, st) : pa_run<float>(a, pl, st);
 }

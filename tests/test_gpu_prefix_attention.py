@@ -116,6 +116,35 @@ def test_lengths(P, S, dtype):
     _check(c, dtype, 0.2)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", DIMS)
+def test_heads_and_dimensions_of_longer_caches(Hq, Hkv, D, dtype):
+    # more keys than one block takes for a row: splits and their join
+    c, _ = _case(dtype, [0, 3, 4, 9], 9, Hq, Hkv, D, 570, 37, D + Hq)
+    _check(c, dtype, D ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S", [19, 540])
+def test_few_keys_of_the_capacity(S, dtype):
+    # the same lengths, from none to a few steps, in caches whose capacity is short
+    # (a block a row) and long (splits, most without a key)
+    c, _ = _case(dtype, [0, 1, 2, 4, 5, 9, 12], 12, 4, 2, 64, 160, S, 3)
+    c["pl"][:] = [0, 1, 15, 31, 33, 100]
+    c["sl"][:] = [0, 1, 16, 17, 5, 0, 19, 2, 18, 1, 0, 8]
+    _check(c, dtype, 0.2)
+
+
+@pytest.mark.parametrize("P,S", [(512, 0), (511, 1), (480, 32), (513, 0), (481, 32), (0, 512),
+                                 (256, 0), (225, 31)])
+def test_capacities_about_the_limit_of_one_block(P, S):
+    for dtype, D in (("bf16", 64), ("bf16", 256), ("f32", 64)):
+        c, _ = _case(dtype, [0, 2, 3], 3, 2, 1, D, P, S, P + S)
+        _check(c, dtype, 0.1)
+        c["pl"][:], c["sl"][:] = P, S
+        _check(c, dtype, 0.1)
+
+
 @pytest.mark.parametrize("rows,Hq,Hkv", [(1, 2, 2), (9, 2, 1), (17, 8, 2), (64, 4, 1), (130, 2, 1)])
 def test_shared_by_many_rows(rows, Hq, Hkv):
     # one to seventeen tiles of sixteen query columns behind one prefix
