@@ -113,8 +113,9 @@ int moe_layer_decode(const void* x, int32_t dtype, int64_t T, int64_t H, const v
  *   c(b, v)  = scores[b] + logits[b, v] - ln sum_u exp logits[b, u]
  *   a beam with finished[b] != 0 has one continuation only: (b, eos) with
  *   c = scores[b], whatever its logits hold
- *   result   the n_out largest c, descending; equal ones lower beam first,
- *            then lower token
+ *   result   the n_out largest c, descending; equal ones lower beam first; within
+ *            a beam larger logit first, then lower token (a score so large that
+ *            sums of different logits are equal does not change their order)
  *
  * A continuation counts when its c is a number above -inf: rows whose logits
  * hold a NaN or +inf, tokens of logit -inf and beams of score -inf have none.

@@ -4,7 +4,9 @@ paper runs on translation and summarisation, Sec. 4.1).
 
 c(b, v) = score_b + logits[b, v] - ln sum_u exp logits[b, u]; a finished beam
 continues only with the end token, at its score. Candidates that are NaN or
--inf do not count; equal ones go to the lower beam, then the lower token."""
+-inf do not count; equal ones go to the lower beam. Within a beam the order is that
+of the logits, then of the tokens (the lower first), also where float64 sums of
+different logits are equal."""
 import numpy as np
 
 
@@ -24,7 +26,7 @@ def beam_select(logits, scores, n_out, finished=None, eos=None):
             s = scores[b, k]
             if finished is not None and finished[b, k]:
                 if s > -np.inf:
-                    cand.append((-s, k, eos))
+                    cand.append((-s, k, 0.0, eos))
                 continue
             z = logits[b, k]
             if not np.isfinite(s) and not s > 0:           # -inf, NaN
@@ -35,11 +37,11 @@ def beam_select(logits, scores, n_out, finished=None, eos=None):
             lse = m + np.log(np.sum(np.exp(z - m)))
             c = s + (z - lse)
             # the n_out best of a row are enough; a stable sort keeps low tokens first
-            for v in np.argsort(-c, kind="stable")[:n_out]:
+            for v in np.argsort(-z, kind="stable")[:n_out]:
                 if c[v] > -np.inf:
-                    cand.append((-c[v], k, int(v)))
+                    cand.append((-c[v], k, -z[v], int(v)))
         cand.sort()
-        for j, (c, k, v) in enumerate(cand[:n_out]):
+        for j, (c, k, _, v) in enumerate(cand[:n_out]):
             parent[b, j], token[b, j], score[b, j] = b * K + k, v, -c
             if eos is not None:
                 done[b, j] = int(v == eos or bool(finished is not None and finished[b, k]))

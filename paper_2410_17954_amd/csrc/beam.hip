@@ -8,7 +8,9 @@
 // the lists.
 // Keys are (value, index) pairs, larger value first, lower index among equal
 // values: no two are equal, which bounds how many can lie above a threshold
-// whatever the logits hold.
+// whatever the logits hold. A merge's index is the beam, then the logit, larger
+// first, then the token: beside a large score float64 sums of different logits are
+// equal, and only with the logit in it is the order that of the chunks' lists.
 #include "moeflow_decode.h"
 #include "common.h"
 #include "buffers.h"
@@ -27,6 +29,7 @@ constexpr int kSelMaxBeams = 32, kSelMaxOut = 64;
 constexpr int kMergeThreads = 512;
 constexpr int kMergeCopy = 4096;                 // keys that a merge keeps in LDS
 constexpr int kMergeLists = 4096 + kSelMaxBeams; // lists of a request, keys that reach a threshold
+constexpr uint64_t kNoPos = ~0ull;               // behind every key
 
 struct SelLayout {
   size_t stat, val, idx, total;
@@ -53,8 +56,8 @@ SelLayout sel_layout(int64_t B, int32_t K, int64_t V, int32_t n_out) {
   return s;
 }
 
-template <typename V>
-__device__ __forceinline__ bool ahead(V a, int32_t ai, V b, int32_t bi) {
+template <typename V, typename I>
+__device__ __forceinline__ bool ahead(V a, I ai, V b, I bi) {
   return (a > b) | ((a == b) & (ai < bi));       // no branch, behind which a load would wait
 }
 
@@ -306,13 +309,13 @@ beam_rows_kernel(const Tv* __restrict__ logits, int64_t V, const int32_t* __rest
 
 // rank[i] = keys ahead of key i, for i < count, by the whole block: as many threads
 // share a key as there are. rank is zero on entry; ends with a barrier.
-__device__ __forceinline__ void merge_ranks(const double* key, const int32_t* pos, int count,
+__device__ __forceinline__ void merge_ranks(const double* key, const uint64_t* pos, int count,
                                             int32_t* rank) {
   const int per = max(1, kMergeThreads / max(count, 1));
   for (int q = threadIdx.x; q < count * per; q += kMergeThreads) {
     const int i = q % count, p = q / count;
     const double c = key[i];
-    const int32_t at = pos[i];
+    const uint64_t at = pos[i];
     int r = 0;
 #pragma unroll 4
     for (int o = count * p / per; o < count * (p + 1) / per; ++o) r += ahead(key[o], pos[o], c, at);
@@ -334,14 +337,14 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
                   int32_t* __restrict__ token, float* out_scores,
                   int32_t* out_finished) {
   __shared__ double s_key[kMergeLists];          // first keys, then the keys to rank
-  __shared__ int32_t s_pos[kMergeLists];         // beam << 25 | token: in the order of both
+  __shared__ uint64_t s_pos[kMergeLists];        // beam << 57 | logit << 25 | token, in order
   __shared__ int32_t s_rank[kMergeLists];
   __shared__ float c_val[kMergeCopy];
   __shared__ int32_t c_idx[kMergeCopy];
   __shared__ double s_off[kSelMaxBeams];         // score - lse, or the score of a finished beam
   __shared__ int s_done[kSelMaxBeams];
   __shared__ double s_thr;
-  __shared__ int32_t s_thr_pos;
+  __shared__ uint64_t s_thr_pos;
   __shared__ int s_count;
   const int64_t b = blockIdx.x;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
@@ -361,7 +364,7 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
   }
   if (threadIdx.x == 0) {
     s_thr = -INFINITY;
-    s_thr_pos = 0x7fffffff;
+    s_thr_pos = kNoPos;
     s_count = 0;
   }
   for (int l = threadIdx.x; l < kMergeLists; l += kMergeThreads) s_rank[l] = 0;
@@ -401,10 +404,11 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
   }
   __syncthreads();
   // key j of list l of beam k; the single key of a finished beam is in its first list
-  auto key = [&](int k, int l, int j, double& c, int32_t& pos) {
+  auto key = [&](int k, int l, int j, double& c, uint64_t& pos) {
     c = -INFINITY;
-    pos = 0x7fffffff;
+    pos = kNoPos;
     int t = -1;
+    float z = 0.f;                               // a finished beam has one key
     if (s_done[k]) {
       if (l == k * chunks && j == 0) {
         c = s_off[k];
@@ -413,14 +417,17 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
     } else {
       const int at = l * n + j;
       t = copied ? c_idx[at] : g_idx[at];
-      if (t >= 0) c = (double)(copied ? c_val[at] : g_val[at]) + s_off[k];
+      if (t >= 0) {
+        z = copied ? c_val[at] : g_val[at];
+        c = (double)z + s_off[k];
+      }
     }
     if (t < 0 || !(c > -INFINITY)) c = -INFINITY;          // NaN too
-    else pos = k << 25 | t;
+    else pos = (uint64_t)k << 57 | (uint64_t)~float_order(z) << 25 | (uint32_t)t;
   };
   for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
     double c;
-    int32_t pos;
+    uint64_t pos;
     key(l / chunks, l, 0, c, pos);
     s_key[l] = c;
     s_pos[l] = pos;
@@ -437,13 +444,13 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
     for (int l = threadIdx.x; l < lists; l += kMergeThreads) s_rank[l] = 0;
   }
   const double thr = s_thr;
-  const int32_t thr_pos = s_thr_pos;
+  const uint64_t thr_pos = s_thr_pos;
   // lists of at most n, in descending order, and at most n of them reach the threshold
   for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
     const int k = l / chunks;
     for (int j = 0; j < n; ++j) {
       double c;
-      int32_t pos;
+      uint64_t pos;
       key(k, l, j, c, pos);
       if (!(c > -INFINITY) || c < thr) break;
       if (c == thr && pos > thr_pos) continue;
@@ -465,10 +472,10 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
   merge_ranks(s_key, s_pos, count, s_rank);
   for (int q = threadIdx.x; q < count; q += kMergeThreads) {
     const double c = s_key[q];
-    const int32_t pos = s_pos[q];
+    const uint64_t pos = s_pos[q];
     const int rank = s_rank[q];
     if (rank < n) {
-      const int k = pos >> 25, t = pos & 0x1ffffff;
+      const int k = (int)(pos >> 57), t = (int)(pos & 0x1ffffff);
       put(rank, (int32_t)(b * K + k), t, (float)c, t == eos || s_done[k]);
     }
   }

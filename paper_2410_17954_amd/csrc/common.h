@@ -23,6 +23,13 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(f));
 }
 
+// Float32 bits in an order that unsigned integers compare: larger float first,
+// -0 as +0.
+__device__ __forceinline__ uint32_t float_order(float f) {
+  const uint32_t b = __float_as_uint(f + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;

@@ -169,11 +169,6 @@ struct LdRoutes {
   int32_t n_active;
 };
 
-// Float32 bits in an order that unsigned integers compare: larger float first.
-__device__ __forceinline__ uint32_t float_order(float f) {
-  const uint32_t b = __float_as_uint(f + 0.f);   // -0 as +0
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
 __device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
   v = max(v, (uint32_t)dpp<0xB1>((int)v));
   v = max(v, (uint32_t)dpp<0x4E>((int)v));

@@ -205,3 +205,12 @@ def test_beam_select_in_place_only_where_rows_keep_their_places(lib):
     assert call(n=5) == ops.MOE_ERR_WORKSPACE
     assert call(n=5, best=FAKE) == ops.MOE_ERR_ARG
     assert call(n=3, flags=FAKE) == ops.MOE_ERR_ARG
+
+
+def test_oracle_select_orders_a_beam_by_its_logits():
+    # float64 sums with a score of -1e30 are all equal
+    z = np.array([[[0.0, 2.0, 1.0, 2.0], [5.0, 0.0, 0.0, 9.0]]])
+    for s in (-1e30, np.inf):
+        parent, token, score, _ = oracle.beam_select(z, np.full((1, 2), s), 6)
+        assert parent[0].tolist() == [0, 0, 0, 0, 1, 1] and (score == s).all()
+        assert token[0].tolist() == [1, 3, 2, 0, 3, 0]
