@@ -71,9 +71,11 @@ int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, in
  *   z[t, e]   = x_t . w_router[e] (+ bias), in float64
  *   idx[t, :] = the k largest z[t, :], descending; equal ones go to the lower
  *               expert; a NaN is never chosen (fewer than k numbers: idx -1,
- *               gate 0)
- *   w[t, j]   = softmax(z[t, :])[idx[t, j]], with renormalize divided by their
- *               sum over j
+ *               gate 0), and where no z[t, :] is above -inf (a mask that leaves
+ *               nothing) nothing is: idx -1, gate 0 throughout
+ *   w[t, j]   = softmax(z[t, :])[idx[t, j]] over the z[t, :] that are numbers,
+ *               with renormalize divided by their sum over j; an expert of z -inf
+ *               beside others has gate 0, a z of +inf makes the gates NaN
  *   y[t]      = (accumulate: y[t] +) sum_{j: slot(idx) in 0..S-1} w[t, j] E(x_t)
  *               + Shared(x_t)
  *   E(x)      = w_down . a,  a = silu(w_gate . x) * (w_up . x)

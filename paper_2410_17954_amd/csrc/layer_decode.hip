@@ -176,7 +176,8 @@ __device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
   return max(v, (uint32_t)dpp<0x140>((int)v));
 }
 
-// Top-k (larger logit, then lower expert; a NaN is never chosen) of token t by
+// Top-k (larger logit, then lower expert; a NaN is never chosen nor part of the
+// softmax; a token without a logit above -inf chooses nothing) of token t by
 // the 16 lanes of a row; lane gl holds the logits of experts gl + 16 r. k rounds
 // of row maximum over the logits' float32 roundings, whose order is that of the
 // float64 logits wherever they differ; a round in which lanes of some row share
@@ -199,11 +200,12 @@ __device__ __forceinline__ void ld_decide(const double* __restrict__ z, bool liv
   m = fmax(m, dpp<0x4E>(m));
   m = fmax(m, dpp<0x141>(m));
   m = fmax(m, dpp<0x140>(m));
+  if (m == -INFINITY) free = 0;                  // nothing above -inf: no choice
   if (!renorm) {
     float total = 0.f;
 #pragma unroll
     for (int r = 0; r < EPL; ++r)
-      if (live && gl + kRowLanes * r < E) total += expf((float)(v[r] - m));
+      if ((free >> r) & 1) total += expf((float)(v[r] - m));
     total += dpp<0xB1>(total);
     total += dpp<0x4E>(total);
     total += dpp<0x141>(total);

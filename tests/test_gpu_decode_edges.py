@@ -6,8 +6,9 @@ import torch
 
 import oracle
 from paper_2410_17954_amd import ops, synth
-from gpu_helpers import to_dev, to_host
+from gpu_helpers import to_dev, to_host, vals
 from test_gpu_beam import _bound
+from test_gpu_layer_decode import _check, _expert_bound, _f, _inputs
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -48,3 +49,57 @@ def test_scores_that_swallow_the_logits(n, scores, dtype):
         finite = np.isfinite(rs[0])
         assert (score[:, ~finite] == rs[0, ~finite]).all()
         assert (np.abs(score[:, finite] - rs[:, finite]) <= _bound(rs[0, finite], V)).all()
+
+
+def _layer_bound(d, ref, u):
+    """The bound of test_gpu_layer_decode on every output of a layer whose slots are
+    its experts."""
+    x, (wg, wu, wd) = _f(d["x"]), (_f(d[n]) for n in ("w_gate", "w_up", "w_down"))
+    n = ref["idx"].shape[1] * wg.shape[1] + (0 if d["shared"] is None else d["shared"][0].shape[0])
+    bound = u * np.abs(ref["y"]) + 2.0 ** -23 * np.abs(ref["y"])
+    for e in np.unique(ref["idx"]):
+        gate = np.where(ref["idx"] == e, ref["w"], 0).sum(1)[:, None]
+        bound += _expert_bound(x, wg[e], wu[e], wd[e], gate, u, n)
+    if d["shared"] is not None:
+        bound += _expert_bound(x, *(_f(t) for t in d["shared"]), 1.0, u, n)
+    return bound * (1 + u) + 1e-37
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,E,Fs", [(5, 7, 0), (16, 40, 24), (40, 130, 24)])
+def test_routes_of_masks_that_leave_little(T, E, Fs, dtype, renorm):
+    """A NaN logit counts for nothing (as one that a mask pushes down to nothing), a
+    token whose mask leaves no expert has none, and neither touches the others."""
+    H, F, k = 64, 40, 3
+    d, g = _inputs(T, H, F, E, E, dtype, T + E, Fs)
+    args = [to_dev(d[n]) for n in ("x", "w_router", "w_gate", "w_up", "w_down")]
+    sh = None if d["shared"] is None else tuple(to_dev(t) for t in d["shared"])
+
+    def call(bias):
+        return ops.layer_decode(*args, k, bias=to_dev(bias), renormalize=renorm, shared=sh)
+
+    nan = g.standard_normal((T, E)).astype(np.float32)
+    nan[1, [0, E - 2]] = np.nan
+    nan[T - 2, k:] = np.nan                  # k numbers left
+    low = np.where(np.isnan(nan), np.float32(-1e30), nan)
+    masked, _ = _check(d, k, dtype, bias=low, renorm=renorm)
+    for a, b in zip(call(nan), masked):
+        assert torch.equal(a, b)
+    empty, rest = [2, T - 1], [t for t in range(T) if t not in (2, T - 1)]
+    nan[2] = -np.inf                         # nothing left
+    nan[T - 1], nan[T - 1, 4] = -np.inf, np.nan
+    y, idx, w, inc = call(nan)
+    assert torch.equal(idx[rest], masked[1][rest]) and torch.equal(w[rest], masked[2][rest])
+    assert (idx[empty] == -1).all() and (w[empty] == 0).all() and (inc == 0).all()
+    f = {n: _f(d[n]) for n in ("x", "w_router", "w_gate", "w_up", "w_down")}
+    shared = None if sh is None else tuple(_f(t) for t in d["shared"])
+    ref = oracle.moe_layer(f["x"], f["w_router"], k, f["w_gate"], f["w_up"], f["w_down"],
+                           bias=low.astype(np.float64), renormalize=renorm, shared=shared)
+    ref["w"][empty] = 0
+    ref["y"][empty] = 0
+    if shared is not None:
+        a = f["x"][empty] @ shared[0].T
+        ref["y"][empty] = (a / (1 + np.exp(-a)) * (f["x"][empty] @ shared[1].T)) @ shared[2].T
+    u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    assert (np.abs(vals(y) - ref["y"]) <= _layer_bound(d, ref, u)).all()
