@@ -136,6 +136,8 @@ int moe_layer_decode(const void* x, int32_t dtype, int64_t T, int64_t H, const v
  * out_scores    [B, n_out] float32 output
  * out_finished  [B, n_out] int32 output or NULL: 1 when the parent had finished
  *               or token == eos
+ * workspace     moe_beam_select_workspace bytes, 256-byte aligned; a size that does not
+ *               fall as B, K, V or n_out grows: that of the largest call serves all
  * With n_out == K out_scores may be scores and out_finished may be finished; no
  * other output may overlap an input.
  * Limits: B >= 1, 1 <= K <= 32, V >= 1, K * V <= 2^25, 1 <= n_out <= 64,

@@ -37,22 +37,28 @@ struct SelLayout {
   int ept;                                       // logits a thread takes
 };
 
-// 64, or 8 while longer chunks would leave compute units idle and a merge can take
-// the lists.
+// 64, or 8 while longer chunks would leave compute units idle: K times the short
+// chunks are then below 8 * 256, lists that a merge can take. Small calls have more
+// chunks than larger ones for it, so `total` allows every call for as many as any of
+// fewer requests, beams or tokens has, and never falls as a call grows.
 SelLayout sel_layout(int64_t B, int32_t K, int64_t V, int32_t n_out) {
+  constexpr int64_t kIdle = 256;
+  static_assert(8 * kIdle <= kMergeLists, "short chunks of a request");
   SelLayout s{};
-  s.ept = B * K * ceil_div(V, kSelThreads * 64) < 256 &&
-          K * ceil_div(V, kSelThreads * 8) <= kMergeLists ? 8 : 64;
-  s.chunks = ceil_div(V, (int64_t)s.ept * kSelThreads);
-  const size_t lists = (size_t)(B * K * s.chunks);
-  size_t o = 0;
-  s.stat = o;                                    // {ref, sum of exp(z - ref)} of a chunk, double
-  o = align_up(o + lists * 16, 256);
-  s.val = o;                                     // the chunk's best logits, descending
-  o = align_up(o + lists * n_out * 4, 256);
-  s.idx = o;                                     // their tokens, -1 past the last
-  o = align_up(o + lists * n_out * 4, 256);
-  s.total = o;
+  const int64_t n64 = ceil_div(V, kSelThreads * 64), n8 = ceil_div(V, kSelThreads * 8);
+  s.ept = B * K * n64 < kIdle ? 8 : 64;
+  s.chunks = s.ept == 8 ? n8 : n64;
+  auto take = [&](size_t lists) {
+    size_t o = 0;
+    s.stat = o;                                  // {ref, sum of exp(z - ref)} of a chunk, double
+    o = align_up(o + lists * 16, 256);
+    s.val = o;                                   // the chunk's best logits, descending
+    o = align_up(o + lists * n_out * 4, 256);
+    s.idx = o;                                   // their tokens, -1 past the last
+    return align_up(o + lists * n_out * 4, 256);
+  };
+  s.total = take((size_t)std::max(B * K * n64, std::min(B * K * n8, 8 * (kIdle - 1))));
+  take((size_t)(B * K * s.chunks));
   return s;
 }
 

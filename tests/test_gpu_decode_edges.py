@@ -103,3 +103,23 @@ def test_routes_of_masks_that_leave_little(T, E, Fs, dtype, renorm):
         ref["y"][empty] = (a / (1 + np.exp(-a)) * (f["x"][empty] @ shared[1].T)) @ shared[2].T
     u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
     assert (np.abs(vals(y) - ref["y"]) <= _layer_bound(d, ref, u)).all()
+
+
+def test_select_of_a_shrinking_batch_on_one_workspace():
+    """One buffer, sized for the first step, while requests end: long chunks, then
+    short ones (more lists than the long ones had)."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    K, V, n = 8, 128000, 16
+    z = torch.randn((16, K, V), device=DEV, generator=g).bfloat16()
+    s = torch.randn((16, K), device=DEV, generator=g)
+    size = ops.beam_select_workspace(16, K, V, n)
+    guard = torch.full((size + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    ws = guard[2048:2048 + size]
+    first = None
+    for B in (16, 9, 4, 3, 2, 1):
+        parent, token, score, _ = ops.beam_select(z[:B], s[:B], n, workspace=ws)
+        if first is None:
+            first = parent, token, score
+        assert torch.equal(parent, first[0][:B]) and torch.equal(token, first[1][:B])
+        assert (score - first[2][:B]).abs().max() < 1e-5
+    assert (guard[:2048] == 0x5a).all() and (guard[2048 + size:] == 0x5a).all()
