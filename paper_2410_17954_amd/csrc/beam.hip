@@ -31,6 +31,10 @@ constexpr int kMergeCopy = 4096;                 // keys that a merge keeps in L
 constexpr int kMergeLists = 4096 + kSelMaxBeams; // lists of a request, keys that reach a threshold
 constexpr uint64_t kNoPos = ~0ull;               // behind every key
 
+// Of a merge: a continuation's sum and its place, beam << 57 | logit << 25 | token in
+// their order, which decides between equal sums. 16 bytes, one LDS read.
+struct alignas(16) SelKey { double c; uint64_t pos; };
+
 struct SelLayout {
   size_t stat, val, idx, total;
   int64_t chunks;                                // of a row, a block each
@@ -315,16 +319,17 @@ beam_rows_kernel(const Tv* __restrict__ logits, int64_t V, const int32_t* __rest
 
 // rank[i] = keys ahead of key i, for i < count, by the whole block: as many threads
 // share a key as there are. rank is zero on entry; ends with a barrier.
-__device__ __forceinline__ void merge_ranks(const double* key, const uint64_t* pos, int count,
-                                            int32_t* rank) {
+__device__ __forceinline__ void merge_ranks(const SelKey* key, int count, int32_t* rank) {
   const int per = max(1, kMergeThreads / max(count, 1));
   for (int q = threadIdx.x; q < count * per; q += kMergeThreads) {
     const int i = q % count, p = q / count;
-    const double c = key[i];
-    const uint64_t at = pos[i];
+    const SelKey mine = key[i];
     int r = 0;
 #pragma unroll 4
-    for (int o = count * p / per; o < count * (p + 1) / per; ++o) r += ahead(key[o], pos[o], c, at);
+    for (int o = count * p / per; o < count * (p + 1) / per; ++o) {
+      const SelKey k = key[o];
+      r += ahead(k.c, k.pos, mine.c, mine.pos);
+    }
     if (r) atomicAdd(&rank[i], r);
   }
   __syncthreads();
@@ -342,15 +347,13 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
                   const int32_t* __restrict__ idx, int32_t* __restrict__ parent,
                   int32_t* __restrict__ token, float* out_scores,
                   int32_t* out_finished) {
-  __shared__ double s_key[kMergeLists];          // first keys, then the keys to rank
-  __shared__ uint64_t s_pos[kMergeLists];        // beam << 57 | logit << 25 | token, in order
+  __shared__ SelKey s_key[kMergeLists];          // first keys, then the keys to rank
   __shared__ int32_t s_rank[kMergeLists];
   __shared__ float c_val[kMergeCopy];
   __shared__ int32_t c_idx[kMergeCopy];
   __shared__ double s_off[kSelMaxBeams];         // score - lse, or the score of a finished beam
   __shared__ int s_done[kSelMaxBeams];
-  __shared__ double s_thr;
-  __shared__ uint64_t s_thr_pos;
+  __shared__ SelKey s_thr;
   __shared__ int s_count;
   const int64_t b = blockIdx.x;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
@@ -369,8 +372,7 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
     }
   }
   if (threadIdx.x == 0) {
-    s_thr = -INFINITY;
-    s_thr_pos = kNoPos;
+    s_thr = SelKey{-INFINITY, kNoPos};
     s_count = 0;
   }
   for (int l = threadIdx.x; l < kMergeLists; l += kMergeThreads) s_rank[l] = 0;
@@ -410,9 +412,8 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
   }
   __syncthreads();
   // key j of list l of beam k; the single key of a finished beam is in its first list
-  auto key = [&](int k, int l, int j, double& c, uint64_t& pos) {
-    c = -INFINITY;
-    pos = kNoPos;
+  auto key = [&](int k, int l, int j) {
+    double c = -INFINITY;
     int t = -1;
     float z = 0.f;                               // a finished beam has one key
     if (s_done[k]) {
@@ -428,43 +429,27 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
         c = (double)z + s_off[k];
       }
     }
-    if (t < 0 || !(c > -INFINITY)) c = -INFINITY;          // NaN too
-    else pos = (uint64_t)k << 57 | (uint64_t)~float_order(z) << 25 | (uint32_t)t;
+    if (t < 0 || !(c > -INFINITY)) return SelKey{-INFINITY, kNoPos};   // NaN too
+    return SelKey{c, (uint64_t)k << 57 | (uint64_t)~float_order(z) << 25 | (uint32_t)t};
   };
-  for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
-    double c;
-    uint64_t pos;
-    key(l / chunks, l, 0, c, pos);
-    s_key[l] = c;
-    s_pos[l] = pos;
-  }
+  for (int l = threadIdx.x; l < lists; l += kMergeThreads) s_key[l] = key(l / chunks, l, 0);
   __syncthreads();
   if (lists > n) {
-    merge_ranks(s_key, s_pos, lists, s_rank);
+    merge_ranks(s_key, lists, s_rank);
     for (int l = threadIdx.x; l < lists; l += kMergeThreads)
-      if (s_rank[l] == n - 1 && s_key[l] > -INFINITY) {    // at most one list
-        s_thr = s_key[l];
-        s_thr_pos = s_pos[l];
-      }
+      if (s_rank[l] == n - 1 && s_key[l].c > -INFINITY) s_thr = s_key[l];   // at most one list
     __syncthreads();
     for (int l = threadIdx.x; l < lists; l += kMergeThreads) s_rank[l] = 0;
   }
-  const double thr = s_thr;
-  const uint64_t thr_pos = s_thr_pos;
+  const SelKey thr = s_thr;
   // lists of at most n, in descending order, and at most n of them reach the threshold
   for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
     const int k = l / chunks;
     for (int j = 0; j < n; ++j) {
-      double c;
-      uint64_t pos;
-      key(k, l, j, c, pos);
-      if (!(c > -INFINITY) || c < thr) break;
-      if (c == thr && pos > thr_pos) continue;
+      const SelKey c = key(k, l, j);
+      if (!(c.c > -INFINITY) || ahead(thr.c, thr.pos, c.c, c.pos)) break;
       const int at = atomicAdd(&s_count, 1);
-      if (at < kMergeLists) {
-        s_key[at] = c;
-        s_pos[at] = pos;
-      }
+      if (at < kMergeLists) s_key[at] = c;
     }
   }
   __syncthreads();
@@ -475,14 +460,13 @@ beam_merge_kernel(int K, int64_t V, int chunks, int n, const float* scores,
     out_scores[b * n + at] = c;
     if (out_finished) out_finished[b * n + at] = fin;
   };
-  merge_ranks(s_key, s_pos, count, s_rank);
+  merge_ranks(s_key, count, s_rank);
   for (int q = threadIdx.x; q < count; q += kMergeThreads) {
-    const double c = s_key[q];
-    const uint64_t pos = s_pos[q];
+    const SelKey c = s_key[q];
     const int rank = s_rank[q];
     if (rank < n) {
-      const int k = (int)(pos >> 57), t = (int)(pos & 0x1ffffff);
-      put(rank, (int32_t)(b * K + k), t, (float)c, t == eos || s_done[k]);
+      const int k = (int)(c.pos >> 57), t = (int)(c.pos & 0x1ffffff);
+      put(rank, (int32_t)(b * K + k), t, (float)c.c, t == eos || s_done[k]);
     }
   }
   for (int q = count + threadIdx.x; q < n; q += kMergeThreads) put(q, -1, -1, -INFINITY, 0);
