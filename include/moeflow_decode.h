@@ -48,7 +48,8 @@ extern "C" {
  * prefix_len [G], suffix_len [R] int32 (clipped to 0..P, 0..S) or NULL (all).
  *                What the caches hold from a length on is not used, be it NaN
  * workspace      moe_prefix_attention_workspace bytes, 256-byte aligned (0 and
- *                NULL when P == S == 0)
+ *                NULL when P == S == 0); a size that does not fall as R, G, P or S
+ *                grows: that of the largest call serves all
  * Limits: R >= 1, 1 <= G <= R, Hq a multiple of Hkv, D a multiple of 8 up to
  *   256, P, S < 2^31, Hkv * D * element size < 2^26, tensors of dtype on 16
  *   bytes, scale finite (below 1e-37 it counts as 0). Errors: MOE_ERR_ARG,
@@ -91,7 +92,8 @@ int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, in
  * y          [T, H] dtype output, may be x; no other overlap is allowed
  * topk_idx, topk_w  [T, k] outputs
  * incomplete [T] int32 output or NULL: 1 when some choice is not resident
- * workspace  moe_layer_decode_workspace bytes, 256-byte aligned
+ * workspace  moe_layer_decode_workspace bytes, 256-byte aligned; a size that does not
+ *            fall as T grows: that of the most tokens serves all
  * Results do not depend on scheduling: sums run in a fixed order.
  * Limits: 1 <= T <= 64, 1 <= k <= min(E, 32), E <= 256; H, F, Fs multiples of 8
  *   (bf16) or 4 (float32), at most 2^22, 2^24, 2^24; tensors of dtype on 16 bytes;

@@ -756,7 +756,19 @@ PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t
   const int64_t keys = dtype == MOE_BF16 ? 32 : 16;
   pl.whole = R * Hkv * pl.tiles_s <= 512 &&
              ceil_div(P, keys) + ceil_div(S, keys) <= 2 * pa_row_waves(pl.dp);
-  const size_t n = (size_t)(pl.splits_p + pl.splits_s) * R * Hq;
+  // Splits change with the rows, and a call may need more of a workspace than a larger
+  // one does. So `total` allows each cache as many rows of splits as any call of fewer
+  // rows, groups or keys can have: with b blocks a split, ceil(want / b) splits of R rows
+  // are at most R + (want - 1) R / b rows, and b is at least R Hkv tiles_s of suffixes,
+  // R Hq / bm of prefixes.
+  auto rows = [&](int64_t keys, int64_t more) {
+    return keys == 0 ? 0 : std::min(R * std::min<int64_t>(ceil_div(keys, 128), 64), R + more);
+  };
+  const bool any_rows = dtype == MOE_BF16 && pl.dp <= 128;
+  const int64_t want_bm =                        // the most of any column class
+      any_rows ? 512 * pa_columns(1, true)
+               : 512 * pa_columns(pa_max_tiles(dtype == MOE_BF16 ? 2 : 4, pl.dp), false);
+  const size_t n = (size_t)(rows(P, want_bm / Hq) + rows(S, 512 / (Hkv * pl.tiles_s))) * Hq;
   pl.o = 0;
   pl.ml = align_up(n * D * 4, 256);
   pl.total = align_up(pl.ml + n * 8, 256);

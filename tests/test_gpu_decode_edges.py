@@ -123,3 +123,21 @@ def test_select_of_a_shrinking_batch_on_one_workspace():
         assert torch.equal(parent, first[0][:B]) and torch.equal(token, first[1][:B])
         assert (score - first[2][:B]).abs().max() < 1e-5
     assert (guard[:2048] == 0x5a).all() and (guard[2048 + size:] == 0x5a).all()
+
+
+@pytest.mark.parametrize("P", [700, 16384])
+def test_attention_of_a_shrinking_batch_on_one_workspace(P):
+    """One buffer, sized for the first step, while sequences end: other column tiles,
+    other splits, more of the buffer for fewer rows."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    R, Hq, Hkv, D, S = 49, 32, 8, 128, 500
+    q, ks, vs, kp, vp = (torch.randn(s, device=DEV, generator=g).bfloat16() for s in (
+        (R, Hq, D), (R, S, Hkv, D), (R, S, Hkv, D), (1, P, Hkv, D), (1, P, Hkv, D)))
+    size = ops.prefix_attention_workspace(R, 1, Hq, Hkv, D, P, S)
+    guard = torch.full((size + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    ws = guard[2048:2048 + size]
+    for n in (49, 48, 33, 32, 31, 17, 16, 15, 5, 4, 2, 1):
+        out, lse = ops.prefix_attention(q[:n], kp, vp, ks[:n], vs[:n], workspace=ws)
+        own, own_lse = ops.prefix_attention(q[:n], kp, vp, ks[:n], vs[:n])
+        assert torch.equal(out, own) and torch.equal(lse, own_lse)
+    assert (guard[:2048] == 0x5a).all() and (guard[2048 + size:] == 0x5a).all()
