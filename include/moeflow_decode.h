@@ -143,7 +143,7 @@ int moe_layer_decode(const void* x, int32_t dtype, int64_t T, int64_t H, const v
  * With n_out == K out_scores may be scores and out_finished may be finished; no
  * other output may overlap an input.
  * Limits: B >= 1, 1 <= K <= 32, V >= 1, K * V <= 2^25, 1 <= n_out <= 64,
- *   B * K < 2^31 / 64. Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED,
+ *   B * K < 2^31 / 64, B < 2^23. Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED,
  *   MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_beam_select_workspace(int64_t B, int32_t K, int64_t V, int32_t n_out);

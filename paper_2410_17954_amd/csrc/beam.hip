@@ -593,8 +593,9 @@ bool sel_ok(int64_t B, int32_t K, int64_t V, int32_t n_out) {
   return B >= 1 && K >= 1 && V >= 1 && n_out >= 1;
 }
 bool sel_supported(int64_t B, int32_t K, int64_t V, int32_t n_out) {
+  // a launch's dimension is below 2^32 threads: a merge block a request
   return K <= kSelMaxBeams && n_out <= kSelMaxOut && V <= ((int64_t)1 << 25) / K &&
-         B < ((int64_t)1 << 31) / 64 / K;
+         B < ((int64_t)1 << 31) / 64 / K && B < ((int64_t)1 << 32) / kMergeThreads;
 }
 
 }  // namespace

@@ -15,6 +15,7 @@ from paper_2410_17954_amd.build import library_path
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "moeflow_decode.h")
 FAKE = ctypes.c_void_p(0x1000)      # never dereferenced: validation fails first
+OTHER = ctypes.c_void_p(0x9000000)
 BIG = 1 << 40
 
 
@@ -214,3 +215,16 @@ def test_oracle_select_orders_a_beam_by_its_logits():
         parent, token, score, _ = oracle.beam_select(z, np.full((1, 2), s), 6)
         assert parent[0].tolist() == [0, 0, 0, 0, 1, 1] and (score == s).all()
         assert token[0].tolist() == [1, 3, 2, 0, 3, 0]
+
+
+def test_select_of_more_requests_than_a_launch_has(lib):
+    # 2^32 threads or more in one dimension are no launch: 512 a request
+    def call(B, K):
+        return lib.moe_beam_select(FAKE, 1, B, K, 3, FAKE, None, 0, 1, FAKE, FAKE, OTHER, None, None,
+                                   BIG, None)
+
+    for K in (1, 2, 3):
+        assert lib.moe_beam_select_workspace((1 << 23) - 1, K, 3, 1) > 0
+        assert call((1 << 23) - 1, K) == ops.MOE_ERR_WORKSPACE
+        assert lib.moe_beam_select_workspace(1 << 23, K, 3, 1) == 0
+        assert call(1 << 23, K) == ops.MOE_ERR_UNSUPPORTED
