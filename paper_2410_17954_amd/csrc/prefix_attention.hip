@@ -712,10 +712,15 @@ pa_join_kernel(PaArgs a, int tpr_shift, int sg_shift) {
 
 struct PaPlan {
   int mt, dp, splits_p, splits_s, tiles_s;
+  int tpr_shift, sg_shift;                       // of the join
   bool rows, whole;                              // whole: a launch of rows, no splits
   int64_t slots_p, blocks_p, blocks_s;
   size_t o, ml, total;
 };
+
+int64_t pa_join_blocks(int64_t R, int64_t Hq, const PaPlan& pl) {
+  return ceil_div(R * Hq, kJoinThreads >> (pl.tpr_shift + pl.sg_shift));
+}
 
 // Column tiles of a key-splitting block: the most that leaves every instance
 // without a spilled register.
@@ -749,6 +754,9 @@ PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t
   pl.splits_s = splits(R * Hkv * pl.tiles_s, S, 512);
   pl.blocks_p = ceil_div(pl.slots_p * pl.splits_p, 8) * 8 * Hkv;
   pl.blocks_s = ceil_div(R * pl.tiles_s * pl.splits_s, 8) * 8 * Hkv;
+  pl.tpr_shift = pl.dp == 64 ? 4 : pl.dp == 128 ? 5 : 6;
+  while (pl.sg_shift < 8 - pl.tpr_shift && (2 << pl.sg_shift) <= pl.splits_p + pl.splits_s)
+    ++pl.sg_shift;
   // a step's loads take some 2.5 us, which two of a wave may cost against a launch and
   // the join; and while the blocks run at once, loads of a shared prefix by each of its
   // rows meet in the caches (4 rows behind 250 keys 9.4 us, split 6.8 + 4.2, behind 777
@@ -788,7 +796,9 @@ bool pa_supported(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int6
   if ((double)G * (double)P * Hkv * D * elt > 4e18 || (double)R * (double)S * Hkv * D * elt > 4e18)
     return false;
   const PaPlan pl = pa_plan(R, G, Hq, Hkv, D, P, S, dtype);
-  return pl.blocks_p + pl.blocks_s < lim && ceil_div(R * Hq, 4) < lim;
+  // a launch's dimension is below 2^32 threads
+  return pl.whole || (pl.blocks_p + pl.blocks_s < 2 * lim / (64 * pa_waves(pl.rows)) &&
+                      pa_join_blocks(R, Hq, pl) < 2 * lim / kJoinThreads);
 }
 
 template <typename Tv, int DP>
@@ -831,11 +841,8 @@ int pa_run(const PaArgs& a, const PaPlan& pl, hipStream_t st) {
                       : pa_launch<Tv, 256>(a, pl, blocks, st);
   }
   if (rc != MOE_OK) return rc;
-  const int shift = a.D <= 64 ? 4 : a.D <= 128 ? 5 : 6;
-  int sg = 0;                                    // log2 of the split groups
-  while (sg < 8 - shift && (2 << sg) <= pl.splits_p + pl.splits_s) ++sg;
-  const unsigned grid = (unsigned)ceil_div(a.R * a.Hq, kJoinThreads >> (shift + sg));
-  pa_join_kernel<Tv><<<dim3(grid), dim3(kJoinThreads), 0, st>>>(a, shift, sg);
+  pa_join_kernel<Tv><<<dim3((unsigned)pa_join_blocks(a.R, a.Hq, pl)), dim3(kJoinThreads), 0, st>>>(
+      a, pl.tpr_shift, pl.sg_shift);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }

@@ -228,3 +228,16 @@ def test_select_of_more_requests_than_a_launch_has(lib):
         assert call((1 << 23) - 1, K) == ops.MOE_ERR_WORKSPACE
         assert lib.moe_beam_select_workspace(1 << 23, K, 3, 1) == 0
         assert call(1 << 23, K) == ops.MOE_ERR_UNSUPPORTED
+
+
+def test_attention_of_more_rows_than_a_launch_has(lib):
+    # blocks of 256 or 512 threads a row and key head
+    def call(R, G, P, s):
+        return lib.moe_prefix_attention(FAKE, 1, R, 32, 32, 64, None, G, FAKE, FAKE, P, None, FAKE,
+                                        FAKE, s, None, 0.1, FAKE, None, None, BIG, None)
+
+    for P, s in ((0, 1), (1, 0), (3, 5)):
+        for R, ok in ((1 << 17, True), (1 << 20, False), (1 << 24, False)):
+            need = lib.moe_prefix_attention_workspace(R, R, 32, 32, 64, P, s, 1)
+            assert (need > 0) == ok
+            assert call(R, R, P, s) == (ops.MOE_ERR_WORKSPACE if ok else ops.MOE_ERR_UNSUPPORTED)
