@@ -161,7 +161,8 @@ int moe_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t K, int
  * there on are neither read nor written.
  *
  * caches    HOST array of n_caches (1..16) DEVICE pointers (not read when
- *           S == 0), no two overlapping, each [L, B*K, S, unit_bytes]:
+ *           S == 0), no two overlapping (MOE_ERR_ARG), each
+ *           [L, B*K, S, unit_bytes]:
  *           S positions of unit_bytes opaque bytes per row and layer (keys, values)
  * parent    [B*K] int32: a row of the same request, or -1 (the row keeps its
  *           state); any other value sets *err and the row keeps its state

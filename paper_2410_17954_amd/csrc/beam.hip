@@ -673,12 +673,17 @@ extern "C" int moe_beam_reorder(void* const* caches, int32_t n_caches, int64_t L
   // bytes of a cache stay below 2^62
   const double bytes = (double)L * (double)B * K * ((double)S + 1.0) * (double)unit_bytes;
   if (bytes > 4e18) return MOE_ERR_UNSUPPORTED;
+  const uintptr_t size = (uintptr_t)(L * B * K * S * unit_bytes);
   ReCaches c{};
   uintptr_t low = (uintptr_t)unit_bytes;         // common alignment of every row
   for (int32_t i = 0; i < n_caches; ++i) {
     if (S == 0) continue;                        // no bytes: only new_lens is written
     MOE_CHECK_ARG(caches[i]);
-    for (int32_t j = 0; j < i; ++j) MOE_CHECK_ARG(caches[i] != caches[j]);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(caches[i]);
+    for (int32_t j = 0; j < i; ++j) {            // blocks would read what others write
+      const uintptr_t other = reinterpret_cast<uintptr_t>(caches[j]);
+      MOE_CHECK_ARG(at + size <= other || other + size <= at);
+    }
     c.base[i] = static_cast<char*>(caches[i]);
     low |= reinterpret_cast<uintptr_t>(caches[i]);
   }

@@ -241,3 +241,12 @@ def test_attention_of_more_rows_than_a_launch_has(lib):
             need = lib.moe_prefix_attention_workspace(R, R, 32, 32, 64, P, s, 1)
             assert (need > 0) == ok
             assert call(R, R, P, s) == (ops.MOE_ERR_WORKSPACE if ok else ops.MOE_ERR_UNSUPPORTED)
+
+
+def test_reorder_refuses_overlapping_caches(lib):
+    # caches of 2 x 8 x 8 x 64 = 0x2000 bytes
+    for at in ((0x10000, 0x11fff), (0x11000, 0x10000), (0x10000, 0x20000, 0x10010),
+               (0x20000, 0x10000, 0x1e001)):
+        caches = (ctypes.c_void_p * len(at))(*at)
+        assert lib.moe_beam_reorder(caches, len(at), 2, 2, 4, 8, 64, FAKE, OTHER,
+                                    ctypes.c_void_p(0x9000), FAKE, None) == ops.MOE_ERR_ARG, at

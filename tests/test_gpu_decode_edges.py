@@ -141,3 +141,18 @@ def test_attention_of_a_shrinking_batch_on_one_workspace(P):
         own, own_lse = ops.prefix_attention(q[:n], kp, vp, ks[:n], vs[:n])
         assert torch.equal(out, own) and torch.equal(lse, own_lse)
     assert (guard[:2048] == 0x5a).all() and (guard[2048 + size:] == 0x5a).all()
+
+
+def test_reorder_of_caches_that_touch():
+    """Keys and values in one allocation, one right behind the other: apart. One that
+    begins inside the other: refused, nothing moved."""
+    both = torch.arange(2 * 2 * 4 * 3 * 16, device=DEV, dtype=torch.int32).view(2, 2, 4, 3, 16)
+    keep = both.clone()
+    parent = torch.tensor([[1, 0], [3, 3]], dtype=torch.int32, device=DEV)
+    flat = both.view(-1)
+    n = both[0].numel()
+    with pytest.raises(ops.MoeError):
+        ops.beam_reorder([flat[:n].view(2, 4, 3, 16), flat[n - 4:2 * n - 4].view(2, 4, 3, 16)], parent)
+    assert torch.equal(both, keep)
+    ops.beam_reorder([both[1], both[0]], parent)
+    assert torch.equal(both, keep[:, :, [1, 0, 3, 3]])
