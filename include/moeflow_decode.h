@@ -168,7 +168,7 @@ int moe_beam_select(const void* logits, int32_t dtype, int64_t B, int32_t K, int
  *           state); any other value sets *err and the row keeps its state
  * lens      [B*K] int32 positions in use per row (clipped to 0..S) or NULL (S)
  * new_lens  [B*K] int32 output or NULL: lens[parent[r]] (lens[r] where the row
- *           keeps its state); must not be lens itself
+ *           keeps its state); must not be lens or parent itself
  * err       int32, set to 1 by a bad parent; the caller clears it
  * Limits: L >= 1, B >= 1, 1 <= K <= 32, S >= 0, unit_bytes >= 1, B*K < 2^31,
  *   S * unit_bytes < 2^31.

@@ -666,7 +666,7 @@ extern "C" int moe_beam_reorder(void* const* caches, int32_t n_caches, int64_t L
   MOE_CHECK_ARG(caches && parent && err);
   MOE_CHECK_ARG(n_caches >= 1 && n_caches <= kReMaxCaches && L >= 1 && B >= 1 && K >= 1 &&
                 S >= 0 && unit_bytes >= 1);
-  MOE_CHECK_ARG(!new_lens || new_lens != lens);
+  MOE_CHECK_ARG(!new_lens || (new_lens != lens && new_lens != parent));
   if (K > kSelMaxBeams || B >= ((int64_t)1 << 31) / K || unit_bytes >= ((int64_t)1 << 31) ||
       S >= ((int64_t)1 << 31) / unit_bytes)      // 32-bit offsets within a row
     return MOE_ERR_UNSUPPORTED;

@@ -250,3 +250,10 @@ def test_reorder_refuses_overlapping_caches(lib):
         caches = (ctypes.c_void_p * len(at))(*at)
         assert lib.moe_beam_reorder(caches, len(at), 2, 2, 4, 8, 64, FAKE, OTHER,
                                     ctypes.c_void_p(0x9000), FAKE, None) == ops.MOE_ERR_ARG, at
+
+
+def test_reorder_refuses_lengths_over_what_it_reads(lib):
+    one = (ctypes.c_void_p * 1)(0x10000)
+    for new in (FAKE, OTHER):
+        assert lib.moe_beam_reorder(one, 1, 2, 2, 4, 8, 64, FAKE, OTHER, new, FAKE,
+                                    None) == ops.MOE_ERR_ARG
