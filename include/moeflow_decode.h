@@ -53,7 +53,7 @@ extern "C" {
  * Limits: R >= 1, 1 <= G <= R, Hq a multiple of Hkv, D a multiple of 8 up to
  *   256, P, S < 2^31, Hkv * D * element size < 2^26, tensors of dtype on 16
  *   bytes, launches below 2^32 threads (R * Hkv * ceil(Hq / Hkv / 16) of some
- *   2^22), scale finite (below 1e-37 it counts as 0). Errors: MOE_ERR_ARG,
+ *   2^22), |scale| up to 2.3e38 (below 1e-37 it counts as 0). Errors: MOE_ERR_ARG,
  *   MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_prefix_attention_workspace(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D,

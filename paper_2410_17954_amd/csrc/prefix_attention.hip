@@ -869,7 +869,7 @@ extern "C" int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int
   MOE_CHECK_ARG(q && out && pa_ok(R, G, Hq, Hkv, D, P, S, dtype));
   MOE_CHECK_ARG((P == 0 || (k_prefix && v_prefix)) && (S == 0 || (k_suffix && v_suffix)));
   MOE_CHECK_ARG(group_offsets || R % G == 0);
-  MOE_CHECK_ARG(isfinite(scale));
+  MOE_CHECK_ARG(isfinite(scale * kLog2e));       // scores are held times log2 e
   if (!pa_supported(R, G, Hq, Hkv, D, P, S, dtype)) return MOE_ERR_UNSUPPORTED;
   uintptr_t bits = 0;
   for (const void* p : {q, k_prefix, v_prefix, k_suffix, v_suffix, static_cast<const void*>(out)})
@@ -898,7 +898,7 @@ extern "C" int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int
   a.nq = Hq / Hkv;
   // never 0, which would make a masked key's score NaN: then the queries are zeros
   const bool none = fabsf(scale) < 1e-37f;
-  a.scale2 = none ? 1.f : std::min(fabsf(scale) * kLog2e, 3e38f);
+  a.scale2 = none ? 1.f : fabsf(scale) * kLog2e;
   a.keep = none ? 0u : ~0u;
   a.flip = none || scale >= 0.f ? 0u : dtype == MOE_BF16 ? 0x80008000u : 0x80000000u;
   a.splits_p = pl.splits_p;

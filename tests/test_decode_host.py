@@ -257,3 +257,15 @@ def test_reorder_refuses_lengths_over_what_it_reads(lib):
     for new in (FAKE, OTHER):
         assert lib.moe_beam_reorder(one, 1, 2, 2, 4, 8, 64, FAKE, OTHER, new, FAKE,
                                     None) == ops.MOE_ERR_ARG
+
+
+def test_attention_refuses_a_scale_beyond_its_scores(lib):
+    # scores are held times log2 e, which float32 does not hold of such a scale
+    def call(scale):
+        return lib.moe_prefix_attention(FAKE, 1, 4, 8, 2, 64, None, 2, FAKE, FAKE, 10, None, None,
+                                        None, 0, None, scale, FAKE, None, None, BIG, None)
+
+    for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
+        assert call(scale) == ops.MOE_ERR_WORKSPACE   # everything but the workspace is right
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert call(scale) == ops.MOE_ERR_ARG
