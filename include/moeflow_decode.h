@@ -34,9 +34,9 @@ extern "C" {
  *   s_i       = scale * q[r, h] . K_i over the keys of head h / (Hq / Hkv):
  *               k_prefix[g, 0 .. prefix_len[g]), k_suffix[r, 0 .. suffix_len[r])
  *   out[r, h] = sum_i softmax(s)_i V_i,  lse[r, h] = ln sum_i exp s_i
- * A row without any key: out 0, lse -inf. Float32 scores, statistics and
- * accumulation; bf16: the softmax numerators are rounded to bf16 for the second
- * product, their sum is not. Results do not depend on scheduling.
+ * A row without any key, or whose scores are all -inf: out 0, lse -inf. Float32
+ * scores, statistics and accumulation; bf16: the softmax numerators are rounded to
+ * bf16 for the second product, their sum is not. Results do not depend on scheduling.
  *
  * q, out         [R, Hq, D] dtype; lse [R, Hq] float32 or NULL
  * group_offsets  [G+1] int32, non-decreasing (clipped to 0..R), or NULL: G equal
@@ -96,10 +96,11 @@ int moe_prefix_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, in
  * workspace  moe_layer_decode_workspace bytes, 256-byte aligned; a size that does not
  *            fall as T grows: that of the most tokens serves all
  * Results do not depend on scheduling: sums run in a fixed order.
- * Limits: 1 <= T <= 64, 1 <= k <= min(E, 32), E <= 256; H, F, Fs multiples of 8
- *   (bf16) or 4 (float32), at most 2^22, 2^24, 2^24; tensors of dtype on 16 bytes;
- *   (T*k*F + T*Fs) values below 2 GiB; else MOE_ERR_UNSUPPORTED (the four calls
- *   take such batches). Errors: MOE_ERR_ARG, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
+ * Limits: T >= 1, 1 <= k <= E <= 256, as for moe_route, else MOE_ERR_ARG; T <= 64,
+ *   k <= 32; H, F, Fs multiples of 8 (bf16) or 4 (float32), at most 2^22, 2^24, 2^24;
+ *   tensors of dtype on 16 bytes; (T*k*F + T*Fs) values below 2 GiB; else
+ *   MOE_ERR_UNSUPPORTED (the four calls take such batches). Other errors:
+ *   MOE_ERR_ARG, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_layer_decode_workspace(int64_t T, int64_t H, int64_t F, int32_t E, int32_t k,
                                   int64_t Fs, int32_t dtype);

@@ -4,7 +4,10 @@
 // Bound by reading the caches once (HBM) while a group's query rows are few.
 // Computed row by row the prefix would be read once per row; here the queries
 // of all rows of a group that read one key head (rows x query heads of it) are
-// the columns of the products, so a key is loaded once for all of them.
+// the columns of the products, so a key is loaded once for a tile of them: up to 64
+// columns, beyond that up to 256 in bfloat16; 16 of D > 128, 32 of float32 with
+// D > 64. The tile is that of an average group: larger ones, and more columns than
+// the widest tile, read the prefix once a tile.
 //   S^T = K Q^T     rows: keys, columns: queries
 //   O^T = V^T P^T   rows: values' dimensions, columns: queries
 // Transposed so, a lane of the MFMA result holds scores of one query for four
@@ -259,7 +262,7 @@ struct PaCore {
                                                 const char* lds) {
     const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
     if constexpr (BF16) {
-      // p is rounded to bf16 (at most 2^-9 of it, for the matrix cores); its
+      // p is rounded to bf16 (at most 2^-8 of it, for the matrix cores); its
       // sum is taken of the float32 values
       bf16x8_t pb[MT];
 #pragma unroll
@@ -760,7 +763,9 @@ PaPlan pa_plan(int64_t R, int64_t G, int32_t Hq, int32_t Hkv, int32_t D, int64_t
   // a step's loads take some 2.5 us, which two of a wave may cost against a launch and
   // the join; and while the blocks run at once, loads of a shared prefix by each of its
   // rows meet in the caches (4 rows behind 250 keys 9.4 us, split 6.8 + 4.2, behind 777
-  // 16.6, 7.2 + 4.5; 64 rows of eight key heads 17.3, 16.3 + 4.1; 256 rows 63, 45 + 6.6)
+  // 16.6, 7.2 + 4.5; 64 rows of eight key heads 17.3, 16.3 + 4.1; 256 rows 63, 45 + 6.6).
+  // At the limit the kernels are level (one or four rows behind 480 keys 12.0 and 12.4,
+  // split 6.8 + 4.8 and 6.8 + 4.5), and the launch saved is the gain.
   const int64_t keys = dtype == MOE_BF16 ? 32 : 16;
   pl.whole = R * Hkv * pl.tiles_s <= 512 &&
              ceil_div(P, keys) + ceil_div(S, keys) <= 2 * pa_row_waves(pl.dp);

@@ -156,3 +156,30 @@ def test_reorder_of_caches_that_touch():
     assert torch.equal(both, keep)
     ops.beam_reorder([both[1], both[0]], parent)
     assert torch.equal(both, keep[:, :, [1, 0, 3, 3]])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,P,S", [(2, 30, 5), (3, 900, 40), (70, 300, 3), (40, 0, 20)])
+def test_rows_whose_scores_are_all_minus_infinity(rows, P, S, dtype):
+    """As rows without a key, beside rows whose suffix has one key left."""
+    g = torch.Generator(device=DEV).manual_seed(P)
+    Hq, Hkv, D = 8, 2, 64
+    q, ks, vs, kp, vp = (torch.randn(s, device=DEV, generator=g).to(dtype) for s in (
+        (rows, Hq, D), (rows, S, Hkv, D), (rows, S, Hkv, D), (1, P, Hkv, D), (1, P, Hkv, D)))
+    q[..., 0] = 1.0
+    kp[..., 0], ks[..., 0] = -float("inf"), -float("inf")
+    ks[1::2, S - 1, :, 0] = 0.0
+    prefix = (kp, vp) if P else (None, None)
+    out, lse = ops.prefix_attention(q, *prefix, ks, vs)
+    assert (out[::2] == 0).all() and (lse[::2] == -float("inf")).all()
+    # The only key that counts: its value. The exponential is that of the rounding of its
+    # own score, p = 2^r, |r| below 2^-24 of a score of at most 64 (log2), so p need not
+    # be one. float32: (p v) (1 / p) with a product of the matrix cores (2^-23, either
+    # way), a division and a product (2^-24 each), 2^-22 together. bf16: p is 1 as an
+    # operand, and 1 / p is within 2^-17 of 1, which a value of eight bits rounds to itself.
+    want = vs[1::2, S - 1].repeat_interleave(Hq // Hkv, 1)
+    tol = 0.0 if dtype == torch.bfloat16 else 2.0 ** -22
+    assert ((out[1::2].double() - want.double()).abs() <= tol * want.double().abs()).all()
+    s = (q[1::2].double() * ks[1::2, S - 1].double().repeat_interleave(Hq // Hkv, 1)).sum(-1) / 8
+    # a float32 sum of 64 products of at most 20 each, times log2 e and back
+    assert (lse[1::2] - s).abs().max() <= 2 * 65 * 2.0 ** -24 * 64 * 20 / 8
