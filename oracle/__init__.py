@@ -30,6 +30,8 @@ Modules and the passages they follow:
   rpp       -- forward pass of the routing path predictor of Sec. 3.2
   attention -- attention over a shared prefix and own suffixes
   beam      -- selection over beams and vocabulary, states following their beams
+  prompt    -- causal attention of packed prompts, a cache of 4-bit blocks and the
+               attention over it, log-probabilities of tokens
 """
 from .gating import router_logits, topk_select, softmax, gate_weights, route
 from .permute import permute
@@ -44,6 +46,7 @@ from .layer import moe_layer, dense_ffn, moe_stack, round_bf16, rms_norm
 from .kv import kv_merge, kv_gather, kv_reindex
 from .attention import prefix_attention
 from .beam import beam_select, beam_reorder
+from .prompt import (prompt_attention, kv4_encode, kv4_decode, kv4_attention, token_logprobs)
 from . import rpp
 
 __all__ = [
@@ -55,5 +58,6 @@ __all__ = [
     "plec_order", "plec_run", "lru_run",
     "moe_layer", "dense_ffn", "moe_stack", "round_bf16", "rms_norm",
     "kv_merge", "kv_gather", "kv_reindex", "prefix_attention", "beam_select",
-    "beam_reorder", "rpp",
+    "beam_reorder", "prompt_attention", "kv4_encode", "kv4_decode", "kv4_attention",
+    "token_logprobs", "rpp",
 ]

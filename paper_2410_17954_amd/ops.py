@@ -93,6 +93,16 @@ def load_library(path=None):
         "moe_beam_select_workspace": (SZ, [I64, I32, I64, I32]),
         "moe_beam_select": (I32, [P, I32, I64, I32, I64, P, P, I64, I32, P, P, P, P, P, SZ, P]),
         "moe_beam_reorder": (I32, [P, I32, I64, I64, I32, I64, I64, P, P, P, P, P]),
+        "moe_prompt_attention_workspace": (SZ, [I64, I64, I64, I32, I32, I32, I32]),
+        "moe_prompt_attention": (I32, [P, P, P, I32, I64, I64, I64, I32, I32, I32, I64, I64, I64, P,
+                                       P, ctypes.c_float, P, P, P, SZ, P]),
+        "moe_kv4_store": (I32, [P, P, I32, I64, I32, I32, I64, I64, P, I64, P, P, P, P, P]),
+        "moe_kv4_load": (I32, [P, P, P, P, I64, P, I64, I32, I32, I32, I64, I64, P, P, P]),
+        "moe_kv4_attention_workspace": (SZ, [I64, I64, I32, I32, I32]),
+        "moe_kv4_attention": (I32, [P, I32, I64, I32, I32, I32, P, P, P, P, I64, I64, P, P,
+                                    ctypes.c_float, P, P, P, SZ, P]),
+        "moe_token_logprobs_workspace": (SZ, [I64, I64, I64, I32]),
+        "moe_token_logprobs": (I32, [P, I32, I64, I64, I64, P, I64, I32, P, P, P, P, P, SZ, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -120,6 +130,13 @@ def exported_decode_symbols():
     return ["moe_prefix_attention_workspace", "moe_prefix_attention",
             "moe_layer_decode_workspace", "moe_layer_decode", "moe_beam_select_workspace",
             "moe_beam_select", "moe_beam_reorder"]
+
+
+def exported_prompt_symbols():
+    """The entry points of include/moeflow_prompt.h."""
+    return ["moe_prompt_attention_workspace", "moe_prompt_attention", "moe_kv4_store",
+            "moe_kv4_load", "moe_kv4_attention_workspace", "moe_kv4_attention",
+            "moe_token_logprobs_workspace", "moe_token_logprobs"]
 
 
 def _check(name, status):
@@ -721,11 +738,18 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
 _CURRENT = contextlib.nullcontext()
 
 
-def _one_device(stream, *ts):
-    """Every given tensor contiguous, on one GPU: a context in which that is the
-    current device and `stream`, if there is one, the current stream, so that what
-    the call allocates or fills belongs to the stream that it goes to."""
+def _one_device(stream, *ts, strided=()):
+    """Every given tensor on one GPU, those of ts contiguous: a context in which that
+    is the current device and `stream`, if there is one, the current stream, so that
+    what the call allocates or fills belongs to the stream that it goes to."""
     dev = -1
+    for t in strided:
+        d = t.get_device()
+        if d < 0:
+            raise ValueError("every tensor must be on the GPU")
+        if dev >= 0 and d != dev:
+            raise ValueError("every tensor must be on the same GPU")
+        dev = d
     for t in ts:
         if t is None:
             continue
@@ -969,3 +993,228 @@ def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None
                                   _addr(new_lens), _addr(err), _raw_stream())
     _check("moe_beam_reorder", st)
     return new_lens, err
+
+
+# --------------------------------------------- prompts, a cache in 4 bits, logprobs
+def _token_stride(name, t, heads, width):
+    """Elements between the tokens of t [n, heads, width], whose tokens are packed."""
+    if t.shape[1:] != (heads, width):
+        raise ValueError(f"{name} must be [tokens, {heads}, {width}]")
+    if t.numel() == 0 or t.is_contiguous():
+        return heads * width
+    if (width > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != width):
+        raise ValueError(f"{name}: the heads and channels of a token must be packed")
+    return heads * width if t.shape[0] == 1 else t.stride(0)
+
+
+def prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code=MOE_BF16):
+    return load_library().moe_prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code)
+
+
+def prompt_attention(q, k, v, q_offsets=None, k_offsets=None, scale=None, out=None, lse=None,
+                     want_lse=True, workspace=None, stream=None):
+    """moe_prompt_attention. q [N, Hq, D], k/v [M, Hkv, D], bfloat16 or float32: the
+    packed tokens of all sequences; each may be a slice of a wider buffer (tokens a
+    stride apart). q_offsets, k_offsets int32 [B+1]; without q_offsets there is one
+    sequence; k_offsets None: one sequence, or q_offsets. scale defaults to
+    1/sqrt(D). Returns (out [N, Hq, D], lse float32 [N, Hq] or None)."""
+    torch = _torch()
+    lib = load_library()
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
+        raise ValueError("q must be [N, Hq, D], k and v [M, Hkv, D]")
+    N, Hq, D = q.shape
+    M, Hkv = k.shape[:2]
+    dt = _dtype_code(q)
+    if k.dtype != q.dtype or v.dtype != q.dtype or v.shape[0] != M:
+        raise ValueError("q, k and v must have one dtype, k and v one length")
+    qs = _token_stride("q", q, Hq, D)
+    ks, vs = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
+    B = 1
+    if q_offsets is not None:
+        if q_offsets.dim() != 1 or q_offsets.shape[0] < 2:
+            raise ValueError("q_offsets must be [B+1]")
+        B = q_offsets.shape[0] - 1
+        _want("q_offsets", q_offsets, (B + 1,), torch.int32)
+        if k_offsets is None and B > 1 and M != N:
+            raise ValueError("k_offsets are needed where keys and queries differ")
+    _want("k_offsets", k_offsets, (B + 1,), torch.int32)
+    _want("out", out, (N, Hq, D), q.dtype)
+    _want("lse", lse, (N, Hq), torch.float32)
+    with _one_device(stream, q_offsets, k_offsets, out, lse, workspace, strided=(q, k, v)):
+        if out is None:                # rows of no sequence are left as they are
+            new = torch.empty if q_offsets is None else torch.zeros
+            out = new((N, Hq, D), dtype=q.dtype, device=q.device)
+        if lse is None and want_lse:
+            lse = torch.full((N, Hq), -float("inf"), dtype=torch.float32, device=q.device)
+        ws, nbytes = _scratch(workspace, q.device, lib.moe_prompt_attention_workspace, N, M, B, Hq,
+                              Hkv, D, dt)
+        st = lib.moe_prompt_attention(
+            _addr(q), _addr(k), _addr(v), dt, N, M, B, Hq, Hkv, D, qs, ks, vs, _addr(q_offsets),
+            _addr(k_offsets), float(D ** -0.5 if scale is None else scale), _addr(out), _addr(lse),
+            _addr(ws), nbytes, _raw_stream())
+    _check("moe_prompt_attention", st)
+    return out, lse
+
+
+def kv4_cache(rows, positions, Hkv, D, device):
+    """An empty cache in 4 bits: (k_codes, k_scales, v_codes, v_scales), uint8, codes
+    [rows, positions, Hkv, D // 2] and scales [rows, positions, Hkv, D // 32]. Slot s
+    is position s % positions of row s // positions."""
+    torch = _torch()
+    if D % 32:
+        raise ValueError("D must be a multiple of 32")
+    return tuple(torch.zeros((rows, positions, Hkv, w), dtype=torch.uint8, device=device)
+                 for w in (D // 2, D // 32) * 2)
+
+
+def _kv4_shape(cache):
+    torch = _torch()
+    kc, ks, vc, vs = cache
+    if kc.dim() != 4:
+        raise ValueError("a cache's codes must be [rows, positions, Hkv, D // 2]")
+    C, S, Hkv, half = kc.shape
+    for name, t, w in (("k_codes", kc, half), ("v_codes", vc, half), ("k_scales", ks, half // 16),
+                       ("v_scales", vs, half // 16)):
+        _want(name, t, (C, S, Hkv, w), torch.uint8)
+    return C, S, Hkv, 2 * half
+
+
+def kv4_store(k, v, cache, slots=None, stream=None):
+    """moe_kv4_store: k/v [N, Hkv, D], bfloat16 or float32 (slices of wider buffers may
+    be), into the slots `slots` (int32 [N], None: 0 .. N-1) of a cache as kv4_cache
+    makes it. A negative slot leaves its token out."""
+    torch = _torch()
+    lib = load_library()
+    if k.dim() != 3 or v.dim() != 3 or k.dtype != v.dtype or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v must be [N, Hkv, D] of one dtype")
+    N = k.shape[0]
+    C, S, Hkv, D = _kv4_shape(cache)
+    dt = _dtype_code(k)
+    kst, vst = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
+    _want("slots", slots, (N,), torch.int32)
+    kc, ks, vc, vs = cache
+    with _one_device(stream, *cache, slots, strided=(k, v)):
+        st = lib.moe_kv4_store(_addr(k), _addr(v), dt, N, Hkv, D, kst, vst, _addr(slots), C * S,
+                               _addr(kc), _addr(ks), _addr(vc), _addr(vs), _raw_stream())
+    _check("moe_kv4_store", st)
+
+
+def kv4_load(cache, slots=None, k=None, v=None, dtype=None, stream=None):
+    """moe_kv4_load: the slots `slots` (int32 [N], None: as many as k has, else all) of
+    a cache as values. k/v [N, Hkv, D] may be slices of wider buffers; new ones are of
+    `dtype` (bfloat16 unless given). Returns (k, v); tokens of a negative slot keep what
+    k and v hold (zeros in new ones)."""
+    torch = _torch()
+    lib = load_library()
+    C, S, Hkv, D = _kv4_shape(cache)
+    if (k is None) != (v is None):
+        raise ValueError("keys and values go together")
+    N = slots.shape[0] if slots is not None else k.shape[0] if k is not None else C * S
+    _want("slots", slots, (N,), torch.int32)
+    if k is not None:
+        if k.dim() != 3 or v.dim() != 3 or k.dtype != v.dtype or k.shape[0] != N or v.shape[0] != N:
+            raise ValueError("k and v must be [N, Hkv, D] of one dtype")
+        if dtype is not None and dtype != k.dtype:
+            raise ValueError("dtype differs from that of k and v")
+    kc, ks, vc, vs = cache
+    with _one_device(stream, *cache, slots, strided=() if k is None else (k, v)):
+        if k is None:
+            new = torch.empty if slots is None else torch.zeros
+            k, v = (new((N, Hkv, D), dtype=dtype or torch.bfloat16, device=kc.device)
+                    for _ in range(2))
+        dt = _dtype_code(k)
+        kst, vst = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
+        st = lib.moe_kv4_load(_addr(kc), _addr(ks), _addr(vc), _addr(vs), C * S, _addr(slots), N,
+                              Hkv, D, dt, kst, vst, _addr(k), _addr(v), _raw_stream())
+    _check("moe_kv4_load", st)
+    return k, v
+
+
+def kv4_attention_workspace(R, S, Hq, Hkv, D):
+    return load_library().moe_kv4_attention_workspace(R, S, Hq, Hkv, D)
+
+
+def kv4_attention(q, cache, lens=None, cache_row=None, scale=None, out=None, lse=None,
+                  want_lse=True, workspace=None, stream=None):
+    """moe_kv4_attention: q [R, Hq, D], one token a row, over a cache as kv4_cache makes
+    it; row r reads the first lens[r] (int32 [R], None: all) positions of the cache's row
+    cache_row[r] (int32 [R], None: r). scale defaults to 1/sqrt(D). Returns
+    (out [R, Hq, D], lse float32 [R, Hq] or None)."""
+    torch = _torch()
+    lib = load_library()
+    if q.dim() != 3:
+        raise ValueError("q must be [R, Hq, D]")
+    R, Hq, D = q.shape
+    C, S, Hkv, width = _kv4_shape(cache)
+    if width != D:
+        raise ValueError("q and the cache differ in D")
+    dt = _dtype_code(q)
+    _want("lens", lens, (R,), torch.int32)
+    _want("cache_row", cache_row, (R,), torch.int32)
+    _want("out", out, (R, Hq, D), q.dtype)
+    _want("lse", lse, (R, Hq), torch.float32)
+    kc, ks, vc, vs = cache
+    with _one_device(stream, q, *cache, lens, cache_row, out, lse, workspace):
+        if out is None:
+            out = torch.empty_like(q)
+        if lse is None and want_lse:
+            lse = torch.empty((R, Hq), dtype=torch.float32, device=q.device)
+        ws, nbytes = _scratch(workspace, q.device, lib.moe_kv4_attention_workspace, R, S, Hq, Hkv, D)
+        st = lib.moe_kv4_attention(
+            _addr(q), dt, R, Hq, Hkv, D, _addr(kc), _addr(ks), _addr(vc), _addr(vs), C, S,
+            _addr(cache_row), _addr(lens), float(D ** -0.5 if scale is None else scale), _addr(out),
+            _addr(lse), _addr(ws), nbytes, _raw_stream())
+    _check("moe_kv4_attention", st)
+    return out, lse
+
+
+def token_logprobs_workspace(R, V, m, n_top):
+    return load_library().moe_token_logprobs_workspace(R, V, m, n_top)
+
+
+def token_logprobs(logits, tokens=None, n_top=0, logprobs=None, entropy=None, want_entropy=True,
+                   top_tokens=None, top_logprobs=None, workspace=None, stream=None):
+    """moe_token_logprobs. logits [R, V] bfloat16 or float32 (rows may be a stride
+    apart), tokens int32 [R, m] or None. Returns (logprobs float32 [R, m] or None,
+    entropy float32 [R] or None, top_tokens int32 and top_logprobs float32 [R, n_top],
+    None with n_top 0)."""
+    torch = _torch()
+    lib = load_library()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [R, V]")
+    R, V = logits.shape
+    n_top = int(n_top)
+    dt = _dtype_code(logits)
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("the logits of a row must be packed")
+    stride = V if R == 1 else logits.stride(0)
+    if tokens is not None and tokens.dim() != 2:
+        raise ValueError("tokens must be [R, m]")
+    m = 0 if tokens is None else tokens.shape[1]
+    _want("tokens", tokens, (R, m), torch.int32)
+    if logprobs is not None and tokens is None:
+        raise ValueError("logprobs need tokens")
+    if n_top == 0 and (top_tokens is not None or top_logprobs is not None):
+        raise ValueError("top_tokens and top_logprobs need n_top")
+    _want("logprobs", logprobs, (R, m), torch.float32)
+    _want("entropy", entropy, (R,), torch.float32)
+    _want("top_tokens", top_tokens, (R, n_top), torch.int32)
+    _want("top_logprobs", top_logprobs, (R, n_top), torch.float32)
+    with _one_device(stream, tokens, logprobs, entropy, top_tokens, top_logprobs, workspace,
+                     strided=(logits,)):
+        new = lambda t, shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device) \
+            if t is None else t
+        if tokens is not None:
+            logprobs = new(logprobs, (R, m), torch.float32)
+        if want_entropy:
+            entropy = new(entropy, (R,), torch.float32)
+        if n_top > 0:
+            top_tokens = new(top_tokens, (R, n_top), torch.int32)
+            top_logprobs = new(top_logprobs, (R, n_top), torch.float32)
+        ws, nbytes = _scratch(workspace, logits.device, lib.moe_token_logprobs_workspace, R, V, m,
+                              n_top)
+        st = lib.moe_token_logprobs(_addr(logits), dt, R, V, stride, _addr(tokens), m, n_top,
+                                    _addr(logprobs), _addr(entropy), _addr(top_tokens),
+                                    _addr(top_logprobs), _addr(ws), nbytes, _raw_stream())
+    _check("moe_token_logprobs", st)
+    return logprobs, entropy, top_tokens, top_logprobs

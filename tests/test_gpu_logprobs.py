@@ -1,0 +1,147 @@
+"""moe_token_logprobs against the float64 oracle. Top tokens are exact. With d = z - m
+of at most |d| and 2^-24 (|d| log2 e + 3) off an exponential (its argument is rounded,
+the exponential is off by an ulp), sums of up to 32 float32 terms:
+* |d ln S| <= sum p |d| 2^-23 + 36 * 2^-24, and a logprob is rounded once more;
+* the entropy's second sum is off by that relative to its terms p |d|, |d| rounded too."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2410_17954_amd import ops, synth
+from gpu_helpers import to_dev, to_host
+from prompt_helpers import values
+
+pytestmark = pytest.mark.gpu
+MIN = {"bf16": -3.3895313892515355e38, "f32": -3.4028234663852886e38}
+
+
+def _cast(z, dtype):
+    return synth.bf16_bits(z.astype(np.float32)) if dtype == "bf16" else z.astype(np.float32)
+
+
+def _same(got, ref, bound):
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    inf = np.isinf(ref) | (np.abs(ref) > 3.4028235e38)
+    assert np.array_equal(got[inf] < 0, ref[inf] < 0) and np.isinf(got[inf]).all()
+    ok = ~np.isnan(ref) & ~inf
+    err = np.abs(got - ref)[ok]
+    assert (err <= np.broadcast_to(bound, ref.shape)[ok]).all(), err.max()
+
+
+def _check(z, tokens, n_top, logits=None, **kw):
+    """z: host logits as given; tokens [R, m] or None."""
+    R, V = z.shape
+    x = values(z)
+    t = np.zeros((R, 0), np.int64) if tokens is None else tokens
+    with np.errstate(invalid="ignore", over="ignore"):
+        rl, re, rt, rtl = oracle.token_logprobs(x, t, n_top)
+        m = np.where(np.isfinite(x), x, -np.inf).max(1)
+        d = np.where(np.isfinite(x), m[:, None] - x, 0.0)
+        p = np.where(np.isfinite(x), np.exp(-d), 0.0)
+        p = p / np.maximum(p.sum(1, keepdims=True), 1e-300)
+        pd = np.where(p > 0, p * d, 0.0)
+    e_lse = (pd.sum(1) * 2.0 ** -23 + 36 * 2.0 ** -24)
+    e_h = e_lse * 2 + (pd * np.where(p > 0, d, 0) ).sum(1) * 2.0 ** -23 + pd.sum(1) * 40 * 2.0 ** -24
+    got = ops.token_logprobs(to_dev(z) if logits is None else logits,
+                             None if tokens is None else to_dev(tokens.astype(np.int32)), n_top, **kw)
+    lp, en, tt, tl = (None if a is None else to_host(a) for a in got)
+    one = lambda ref: 2.0 ** -23 * np.abs(np.where(np.isfinite(ref), ref, 0.0))
+    if tokens is not None:
+        _same(lp, rl, e_lse[:, None] + one(rl))
+    if en is not None:
+        _same(en, re, e_h + one(re))
+    if n_top:
+        assert np.array_equal(tt, rt)
+        _same(tl, rtl, e_lse[:, None] + one(rtl))
+    else:
+        assert tt is None and tl is None
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V,m,n", [(1, 1, 1, 1), (3, 2, 2, 5), (1, 100, 1, 0), (5, 999, 3, 20),
+                                     (2, 2048, 1, 1), (2, 2049, 1, 64), (7, 4095, 2, 8), (1, 32000, 1, 5),
+                                     (3, 16385, 0, 3), (4, 50257, 5, 16), (2, 152000, 1, 64),
+                                     (300, 3001, 1, 2), (1, 1 << 20, 1, 33)])
+def test_shapes(R, V, m, n, dtype):
+    g = np.random.default_rng(V + n)
+    z = _cast(2.5 * g.standard_normal((R, V)), dtype)
+    _check(z, g.integers(0, V, (R, m)) if m else None, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [70, 5000, 40000])
+def test_ties_and_order(V, dtype):
+    g = np.random.default_rng(V)
+    z = np.zeros((6, V))
+    z[1] = g.integers(-2, 3, V)                      # many equal ones
+    z[2] = np.arange(V)[::-1] / V                    # sorted
+    z[3] = np.arange(V) / V
+    z[4, V // 2:] = 3.0                              # the best all in the last half
+    z[5] = np.where(np.arange(V) % 2, 0.0, -0.0)     # zeros of both signs are equal
+    for n in (1, 5, 64):
+        _check(_cast(z, dtype), g.integers(0, V, (6, 2)), n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [60, 3000, 33000])
+def test_masks_infinities_and_nan(V, dtype):
+    g = np.random.default_rng(V)
+    z = 2.5 * g.standard_normal((12, V))
+    tok = g.integers(0, V, (12, 4))
+    z[0] = -np.inf                                   # nothing left
+    z[1, :] = -np.inf
+    z[1, V - 1] = 2.0                                # one token left
+    z[2, V // 3:] = -np.inf
+    z[3, 1:] = MIN[dtype]                            # masked with the lowest number
+    z[4] = MIN[dtype]
+    z[5, 7] = np.nan
+    z[6, V - 1] = np.inf
+    z[7, 3], z[7, 4:] = np.nan, -np.inf
+    z[8] = 3e38 * np.sign(z[8])                      # differences beyond float32
+    z[9] *= 1e4
+    z[10, ::2] = -np.inf
+    z[11] = -np.inf
+    z[11, [5, V // 2, V - 2]] = [1.0, 1.0, 0.5]      # fewer than the places
+    tok[:, 1], tok[:, 2] = -1, V                     # padding
+    tok[2, 0], tok[3, 0], tok[11, 0] = V - 1, 2, 6   # masked ones
+    for n in (0, 4, 50):
+        _check(_cast(z, dtype), tok, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strided_rows_and_odd_addresses(dtype):
+    g = np.random.default_rng(9)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    for V, stride, at in ((1000, 1003, 1), (33001, 33007, 3), (5, 9, 2)):
+        z = _cast(g.standard_normal((4, V)), dtype)
+        buf = torch.full((4 * stride + at,), float("nan"), dtype=t, device="cuda:0")
+        view = buf.as_strided((4, V), (stride, 1), at)
+        view.copy_(to_dev(z))
+        _check(z, g.integers(0, V, (4, 2)), 5, logits=view)
+
+
+def test_outputs_given_and_left_out():
+    g = np.random.default_rng(2)
+    z, tok = _cast(g.standard_normal((3, 500)), "f32"), g.integers(0, 500, (3, 2))
+    d = "cuda:0"
+    bufs = dict(logprobs=torch.zeros(3, 2, device=d), entropy=torch.zeros(3, device=d),
+                top_tokens=torch.zeros(3, 4, dtype=torch.int32, device=d),
+                top_logprobs=torch.zeros(3, 4, device=d),
+                workspace=ops.workspace_tensor(max(1, ops.token_logprobs_workspace(3, 500, 2, 4)), d))
+    got = _check(z, tok, 4, **bufs)
+    assert got[0] is bufs["logprobs"] and got[1] is bufs["entropy"]
+    assert got[2] is bufs["top_tokens"] and got[3] is bufs["top_logprobs"]
+    assert _check(z, None, 3, want_entropy=False)[:2] == (None, None)
+    assert _check(z, None, 0)[0] is None
+
+
+def test_results_repeat():
+    g = np.random.default_rng(7)
+    z = to_dev(_cast(g.standard_normal((9, 90000)), "bf16"))
+    tok = to_dev(g.integers(0, 90000, (9, 1)).astype(np.int32))
+    a = ops.token_logprobs(z, tok, 10)
+    for _ in range(3):
+        assert all(torch.equal(x, y) for x, y in zip(a, ops.token_logprobs(z, tok, 10)))
