@@ -1,0 +1,168 @@
+// What the attention kernels over packed prompts and over a cache in 4 bits share:
+// tiles of S^T = K Q^T and O^T = V^T P^T on 16x16 MFMAs, where lane (r, q4) = (lane %
+// 16, lane / 16) holds scores of query r for keys 4 q4 .. 4 q4 + 3, the running
+// softmax over them, and the join of key ranges that blocks took.
+#pragma once
+
+#include "common.h"
+
+#include <math.h>
+
+namespace moe {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float quad_max(float v) {   // over the four lanes of a query
+  v = fmaxf(v, __shfl_xor(v, 16, kWave));
+  return fmaxf(v, __shfl_xor(v, 32, kWave));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor(v, 16, kWave);
+  return v + __shfl_xor(v, 32, kWave);
+}
+
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// Scores -> softmax numerators 2^(s scale2 - m) in place, for MT tiles of queries and
+// KT tiles of keys. m: their reference, raised (and l and o rescaled) only where a
+// score exceeds it by more than kSlack, so that most steps rescale nothing and
+// numerators stay below 2^kSlack. One branch for all tiles.
+constexpr float kSlack = 8.f;
+
+template <int MT, int KT, int DT>
+__device__ __forceinline__ void softmax_step(f32x4_t (&s)[MT][KT], float (&m)[MT], float (&l)[MT],
+                                             f32x4_t (&o)[MT][DT], float scale2) {
+  float mx[MT];
+  bool raise = false;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    mx[i] = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx[i] = fmaxf(mx[i], s[i][kt][e]);
+    raise = raise | (mx[i] * scale2 > m[i] + kSlack);
+  }
+  if (ballot(raise)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      mx[i] = quad_max(mx[i]) * scale2;
+      const float to = mx[i] > m[i] + kSlack ? mx[i] : m[i];
+      const float f = to == m[i] ? 1.f : __builtin_amdgcn_exp2f(m[i] - to);   // 0 from -inf
+      m[i] = to;
+      l[i] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[i][dt] *= f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const float mu = m[i] == -INFINITY ? 0.f : m[i];         // nothing but -inf so far
+    float sum = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[i][kt][e], scale2, -mu));
+        s[i][kt][e] = p;
+        sum += p;
+      }
+    l[i] += sum;
+  }
+}
+
+// Four values of a row's result, the row on 16 bytes.
+__device__ __forceinline__ void put4(uint16_t* dst, f32x4_t o) {
+  const uint32_t lo = (uint32_t)f32_to_bf16(o[0]) | (uint32_t)f32_to_bf16(o[1]) << 16;
+  const uint32_t hi = (uint32_t)f32_to_bf16(o[2]) | (uint32_t)f32_to_bf16(o[3]) << 16;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(lo, hi);
+}
+__device__ __forceinline__ void put4(float* dst, f32x4_t o) { *reinterpret_cast<f32x4_t*>(dst) = o; }
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// scale as kernels take it: never 0, which would make a masked key's score NaN; then
+// q & keep ^ flip has no bits, and its signs are turned where scale is negative.
+struct ScoreScale { float scale2; uint32_t keep, flip; };
+inline ScoreScale score_scale(float scale, bool bf16) {
+  const bool none = fabsf(scale) < 1e-37f;
+  return {none ? 1.f : fabsf(scale) * kLog2e, none ? 0u : ~0u,
+          none || scale >= 0.f ? 0u : bf16 ? 0x80008000u : 0x80000000u};
+}
+
+// ---------------------------------------------------------------- join
+// part_o [splits][RH][D], part_ml [splits][RH] (maximum in log2, sum; sum 0: o is not
+// read) -> out [RH, D], lse [RH] of the rows offsets[0] .. offsets[n_off - 1] - 1 (RH /
+// heads rows; all without offsets).
+struct JoinArgs {
+  const float* part_o;
+  const float2* part_ml;
+  const int32_t* offsets;
+  int64_t n_off, RH;
+  int heads, D, splits;
+  void* out;
+  float* lse;
+};
+
+constexpr int kJoinThreads = 256;
+
+// tpr threads (at least D / 4) take four dimensions each of a row and head, sg groups
+// of them share the splits (both powers of two).
+template <typename Tv>
+__global__ void __launch_bounds__(kJoinThreads)
+attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
+  __shared__ f32x4_t s_o[kJoinThreads];
+  __shared__ float2 s_ml[kJoinThreads];
+  const int tpr = 1 << tpr_shift, sg = 1 << sg_shift;
+  const int64_t at = (int64_t)blockIdx.x * (kJoinThreads >> (tpr_shift + sg_shift)) +
+                     (threadIdx.x >> (tpr_shift + sg_shift));
+  const int d = 4 * (threadIdx.x & (tpr - 1)), g = (threadIdx.x >> tpr_shift) & (sg - 1);
+  const int64_t row = at / a.heads;
+  bool live = at < a.RH;
+  if (a.offsets) live = live && row >= a.offsets[0] && row < a.offsets[a.n_off - 1];
+  float m = -INFINITY, l = 0.f;
+  f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const float2 ml, const f32x4_t po) {
+    if (ml.y == 0.f) return;                     // a split without keys wrote no O
+    const float top = fmaxf(m, ml.x), mu = top == -INFINITY ? 0.f : top;
+    const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
+    l = l * f0 + ml.y * f1;
+    o = o * f0 + po * f1;
+    m = top;
+  };
+  if (live && d < a.D) {
+#pragma unroll 4
+    for (int p = g; p < a.splits; p += sg) {
+      const float2 ml = a.part_ml[p * a.RH + at];
+      add(ml, *reinterpret_cast<const f32x4_t*>(a.part_o + (p * a.RH + at) * a.D + d));
+    }
+  }
+  if (sg > 1) {
+    s_o[threadIdx.x] = o;
+    s_ml[threadIdx.x] = make_float2(m, l);
+    __syncthreads();
+    if (g != 0) return;
+    for (int i = 1; i < sg; ++i)                 // in split group order
+      add(s_ml[threadIdx.x + (i << tpr_shift)], s_o[threadIdx.x + (i << tpr_shift)]);
+  }
+  if (!live || d >= a.D) return;
+  o *= l == 0.f ? 0.f : 1.f / l;
+  put4(static_cast<Tv*>(a.out) + at * a.D + d, o);
+  if (a.lse && d == 0) a.lse[at] = lse_of(m, l);
+}
+
+template <typename Tv>
+int attention_join(const JoinArgs& a, hipStream_t st) {
+  const int tpr_shift = a.D <= 64 ? 4 : a.D <= 128 ? 5 : 6;
+  int sg_shift = 0;
+  while (sg_shift < 8 - tpr_shift && (2 << sg_shift) <= a.splits) ++sg_shift;
+  const int64_t blocks = ceil_div(a.RH, kJoinThreads >> (tpr_shift + sg_shift));
+  attention_join_kernel<Tv><<<dim3((unsigned)blocks), dim3(kJoinThreads), 0, st>>>(a, tpr_shift,
+                                                                                  sg_shift);
+  MOE_CHECK_LAUNCH();
+  return MOE_OK;
+}
+
+}  // namespace moe

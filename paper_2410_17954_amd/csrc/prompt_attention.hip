@@ -1,96 +1,404 @@
 // moe_prompt_attention: causal attention of packed sequences.
 //
-// A block takes one query of one head: 256 keys at a time, a thread a score, then a
-// thread a dimension of the values, with the running maximum and sum of the softmax.
+// Bound by the matrix cores where prompts are long: 4 D Hq flop a visible pair of
+// tokens, against K and V read once. The queries of a sequence that read one key head
+// (tokens x query heads of it, so that the tokens a tile spans and with them what the
+// diagonal wastes are few) are the columns of the products:
+//   S^T = K Q^T     rows: keys, columns: queries
+//   O^T = V^T P^T   rows: values' dimensions, columns: queries
+// Transposed so, a lane of the MFMA result holds scores of one query for four
+// neighbouring keys: the running maximum and sum are one register each, the
+// rescaling of O is lane by lane, and the scores of two 16-key tiles are, in
+// place, a lane's eight operands of the second product (its k slots 8q + j are
+// keys 4q + j of the first tile and 4q + j - 4 of the second). V^T comes from LDS
+// through the transposing read, four keys of one column at a time.
+// Every wave has 32 columns of its own; keys and values go straight from memory to LDS,
+// a tile of keys ahead of the one that all waves of a block compute on, swizzled by
+// which 16 bytes each lane fetches. Tiles before the first query of a wave need no
+// mask.
 #include "moeflow_prompt.h"
-#include "common.h"
+#include "attention.h"
+#include "buffers.h"
 #include "spans.h"
-
-#include <math.h>
 
 #include <algorithm>
 
 namespace moe {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kPastEnd = 0xfffffff0u;       // no buffer here is as long
 
 struct PrArgs {
   const void *q, *k, *v;
   const int32_t *q_offsets, *k_offsets;
-  int64_t N, M, B, q_stride, k_stride, v_stride;
-  int Hq, Hkv, D;
-  float scale2;                                  // scale log2 e
+  int64_t N, M, B, q_stride, k_stride, v_stride; // strides in elements
+  int Hq, Hkv, D, nq;                            // nq: query heads of a key head
+  float scale2;                                  // |scale| log2 e
+  uint32_t keep, flip;
+  int splits;
+  int64_t slots;                                 // row tiles (upper bound)
+  float* part_o;                                 // [splits][N * Hq][D]
+  float2* part_ml;                               // [splits][N * Hq]
   void* out;
   float* lse;
 };
-
-__device__ __forceinline__ float as_f32(uint16_t x) { return bf16_to_f32(x); }
-__device__ __forceinline__ float as_f32(float x) { return x; }
-__device__ __forceinline__ void put(uint16_t* p, float x) { *p = f32_to_bf16(x); }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
 
 __device__ __forceinline__ int64_t pr_offset(const int32_t* o, int64_t b, int64_t n) {
   if (!o) return b == 0 ? 0 : n;
   return min(max((int64_t)o[b], (int64_t)0), n);
 }
 
-template <typename Tv>
-__global__ void __launch_bounds__(kThreads) pr_simple_kernel(PrArgs a) {
-  __shared__ float s_q[256], s_p[kThreads], s_red[kThreads / kWave];
-  const int64_t n = blockIdx.x / a.Hq;
-  const int h = (int)(blockIdx.x % a.Hq), hk = h / (a.Hq / a.Hkv), t = threadIdx.x;
-  int64_t lo = 0, hi = a.B;                      // last sequence that starts at or before n
-  while (hi - lo > 1) {
-    const int64_t mid = (lo + hi) / 2;
-    if (pr_offset(a.q_offsets, mid, a.N) <= n) lo = mid;
-    else hi = mid;
+// What a block works on: columns m0 .. m0 + m_n - 1 (column m is token m / nq of the
+// sequence, query head h * nq + m % nq), keys [lo, hi) of the sequence.
+struct PrJob {
+  const char *k, *v;                             // of key 0, head h
+  int64_t row0;                                  // the sequence's first row of q
+  int lo, hi, past, m0, cols;                    // past: keys before the first query's own
+  int h, split;
+};
+
+// Row tiles of sequence b start at slot floor(first row * nq / BM) + b: slots of
+// different sequences never meet, and a wave finds a slot's sequence in steps of 64
+// probes. Later tiles, which see more keys, come first; head h goes to XCD h % 8, so
+// that the tiles of a head share its keys in one L2.
+template <typename Tv, int BM, int BN>
+__device__ __forceinline__ bool pr_find(const PrArgs& a, PrJob& j) {
+  const int64_t u = blockIdx.x;
+  j.h = (int)(u % a.Hkv);
+  j.split = (int)(u / a.Hkv % a.splits);
+  const int64_t slot = a.slots - 1 - u / a.Hkv / a.splits;
+  int64_t b = 0, n = a.B;
+  const int lane = lane_id();
+  while (n > 1) {
+    const int64_t step = (n + 63) / 64, at = b + lane * step;
+    const bool in = at < b + n && pr_offset(a.q_offsets, at, a.N) * a.nq / BM + at <= slot;
+    const int c = max((int)__popcll(ballot(in)) - 1, 0);
+    b += c * step;
+    n = min(step, n - c * step);
   }
-  const int64_t q0 = pr_offset(a.q_offsets, lo, a.N), q1 = pr_offset(a.q_offsets, lo + 1, a.N);
-  if (n < q0 || n >= q1) return;
-  const int64_t k0 = pr_offset(a.k_offsets, lo, a.M);
-  const int64_t k1 = max(k0, pr_offset(a.k_offsets, lo + 1, a.M));
-  const int64_t keys = max((int64_t)0, (k1 - k0) - (q1 - q0) + (n - q0) + 1);
-  const Tv* const q = static_cast<const Tv*>(a.q) + n * a.q_stride + (int64_t)h * a.D;
-  const Tv* const k = static_cast<const Tv*>(a.k) + k0 * a.k_stride + (int64_t)hk * a.D;
-  const Tv* const v = static_cast<const Tv*>(a.v) + k0 * a.v_stride + (int64_t)hk * a.D;
-  if (t < a.D) s_q[t] = as_f32(q[t]);
+  const int64_t r0 = pr_offset(a.q_offsets, b, a.N), r1 = pr_offset(a.q_offsets, b + 1, a.N);
+  const int64_t k0 = pr_offset(a.k_offsets, b, a.M);
+  const int64_t keys = max(pr_offset(a.k_offsets, b + 1, a.M) - k0, (int64_t)0);
+  const int64_t tile = slot - (r0 * a.nq / BM + b);
+  j.cols = (int)((r1 - r0) * a.nq);              // N * Hq < 2^31
+  if (tile < 0 || tile * BM >= j.cols) return false;
+  j.m0 = (int)tile * BM;
+  j.row0 = r0;
+  j.past = (int)(keys - (r1 - r0));
+  const int end = max(j.past + (min(j.m0 + BM, j.cols) - 1) / a.nq + 1, 0);
+  const int per = (int)(((end + (int64_t)a.splits - 1) / a.splits + BN - 1) / BN * BN);
+  j.lo = (int)min((int64_t)end, (int64_t)per * j.split);
+  j.hi = (int)min((int64_t)end, (int64_t)j.lo + per);
+  j.k = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k) + k0 * a.k_stride +
+                                      (int64_t)j.h * a.D);
+  j.v = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v) + k0 * a.v_stride +
+                                      (int64_t)j.h * a.D);
+  return true;
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((ext_vector_type(8))) unsigned short u16x8_t;
+
+// DP: the dimension padded to rows of whole 128 bytes; 16-byte chunks past D are zeros.
+template <typename Tv, int DP, int kMT, int W, int BN>
+struct PrCore {
+  static constexpr bool BF16 = sizeof(Tv) == 2;
+  static constexpr int VE = 16 / sizeof(Tv);     // values per chunk
+  static constexpr int CH = DP / VE;             // chunks of a row
+  static constexpr int QR = CH / 4;              // operands of a query: chunk 4t + q4
+  static constexpr int DT = DP / 16, KT = BN / 16;
+  static constexpr int kTile = BN * CH * 16;     // bytes of a tile of keys, or of values
+  static constexpr int PIECES = kTile / 1024 / W;   // 1 KB pieces a wave loads of a tile
+  static_assert(kTile % (1024 * W) == 0, "whole pieces");
+
+  // Chunk c of row r lies at c ^ swz: sixteen rows' reads of one chunk (keys), and
+  // the transposing reads' eight rows x 32 bytes (values), meet different banks.
+  static __device__ __forceinline__ int swz_k(int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int swz_v(int row) {
+    if constexpr (!BF16) return 4 * ((row >> 2) & 3);
+    return CH == 8 ? 2 * ((row >> 1) & 3) : 2 * (row & 7);
+  }
+  // Byte offsets of the chunks that a lane loads, from a tile's first key on.
+  static __device__ __forceinline__ void offsets(uint32_t (&k)[PIECES], uint32_t (&v)[PIECES],
+                                                 int wave, const PrArgs& a) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int g = (wave * PIECES + p) * 64 + lane_id(), row = g / CH, c = g % CH;
+      const int ck = c ^ swz_k(row), cv = c ^ swz_v(row);
+      k[p] = ck * VE < a.D ? (uint32_t)row * (uint32_t)(a.k_stride * sizeof(Tv)) + ck * 16 : kPastEnd;
+      v[p] = cv * VE < a.D ? (uint32_t)row * (uint32_t)(a.v_stride * sizeof(Tv)) + cv * 16 : kPastEnd;
+    }
+  }
+  // Keys from `key` on into buf, those from `end` on as zeros.
+  static __device__ __forceinline__ void load(char* buf, const char* base, int64_t stride, int key,
+                                              int end, int D, const uint32_t (&off)[PIECES],
+                                              int wave) {
+    const int n = min(end - key, BN);
+    const int64_t row = stride * (int64_t)sizeof(Tv);
+    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(base + key * row), 0,
+        (int)((uint32_t)(n - 1) * (uint32_t)row + (uint32_t)D * sizeof(Tv)), 0x00027000);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          rs, (lds_void*)(buf + (wave * PIECES + p) * 1024), 16, (int)off[p], 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mfma(f32x4_t& c, const u32x4_t& x, const u32x4_t& y) {
+    if constexpr (BF16) {
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x),
+                                                  __builtin_bit_cast(bf16x8_t, y), c, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[v]), __uint_as_float(y[v]), c,
+                                                 0, 0, 0);
+    }
+  }
+  static __device__ __forceinline__ void scores(f32x4_t (&s)[kMT][KT], const u32x4_t (&q)[kMT][QR],
+                                                const char* lds) {
+    const int r = lane_id() & 15, q4 = lane_id() >> 4;
+    const int at = r * CH + (q4 ^ swz_k(r));     // rows 16 apart share swz
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < kMT; ++i) s[i][kt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < QR; ++t) {
+      const char* const from = lds + (at ^ (4 * t)) * 16;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(from + kt * 16 * CH * 16);
+#pragma unroll
+        for (int i = 0; i < kMT; ++i) mfma(s[i][kt], k, q[i][t]);
+      }
+    }
+  }
+  // p, rounded to bf16 (at most 2^-8 of it, for the matrix cores); its sum is taken of
+  // the float32 values
+  static __device__ __forceinline__ u32x4_t numerators(const f32x4_t& p0, const f32x4_t& p1) {
+    bf16x8_t b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      b[e] = (__bf16)p0[e];
+      b[e + 4] = (__bf16)p1[e];
+    }
+    return __builtin_bit_cast(u32x4_t, b);
+  }
+  // O += V^T P^T
+  static __device__ __forceinline__ void values(f32x4_t (&o)[kMT][DT], const f32x4_t (&p)[kMT][KT],
+                                                const char* lds) {
+    const int r = lane_id() & 15, q4 = lane_id() >> 4;
+    if constexpr (BF16) {
+      u32x4_t pb[kMT][KT / 2];
+#pragma unroll
+      for (int i = 0; i < kMT; ++i)
+#pragma unroll
+        for (int g = 0; g < KT / 2; ++g) pb[i][g] = numerators(p[i][2 * g], p[i][2 * g + 1]);
+      const int row = 4 * q4 + (r >> 2), at = row * CH + (((r >> 1) & 1) ^ swz_v(row));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const char* const from = lds + (at ^ (2 * dt)) * 16 + (r & 1) * 8;
+#pragma unroll
+        for (int g = 0; g < KT / 2; ++g) {
+          s16x4_t v[2];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            v[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4_t*)(from + (2 * g + t) * 16 * CH * 16));
+          const u32x4_t vt = __builtin_bit_cast(
+              u32x4_t, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int i = 0; i < kMT; ++i) mfma(o[i][dt], vt, pb[i][g]);
+        }
+      }
+    } else {
+      const int row = 4 * q4, at = row * CH + ((r >> 2) ^ swz_v(row));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const char* const from = lds + (at ^ (4 * dt)) * 16 + (r & 3) * 4;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = *reinterpret_cast<const float*>(from + (16 * kt + e) * CH * 16);
+#pragma unroll
+            for (int i = 0; i < kMT; ++i)
+              o[i][dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p[i][kt][e], o[i][dt], 0, 0, 0);
+          }
+      }
+    }
+  }
+  // Values that are no numbers, in a tile that some query does not see as a whole:
+  // 0 times them would be NaN. Of the chunks that this wave loaded they become 0, and
+  // for every dimension the first key of +inf or NaN and of -inf or NaN is kept: a
+  // query that sees it gets the infinity, or both, at the end.
+  static __device__ __forceinline__ void take_odd(char* tile, int key, int wave, int* up, int* down) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      const int g = (wave * PIECES + p) * 64 + lane_id(), row = g / CH;
+      u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile) + g;
+      const u32x4_t w = *at;
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        odd |= (w[e] & 0x7f800000u) == 0x7f800000u;
+        if constexpr (BF16) odd |= (w[e] & 0x7f80u) == 0x7f80u;
+      }
+      if (!odd) continue;
+      const int d0 = ((g % CH) ^ swz_v(row)) * VE;
+      Tv* const x = reinterpret_cast<Tv*>(at);
+      for (int e = 0; e < VE; ++e) {
+        float f;
+        if constexpr (BF16) f = bf16_to_f32(x[e]);
+        else f = x[e];
+        if (fabsf(f) < INFINITY) continue;
+        if (!(f < 0.f)) atomicMin(up + d0 + e, key + row);
+        if (!(f > 0.f)) atomicMin(down + d0 + e, key + row);
+        x[e] = 0;
+      }
+    }
+  }
+};
+
+constexpr int pr_keys(int elt, int dp) { return elt * dp <= 256 ? 64 : 32; }
+
+// 16-column tiles of a wave: what leaves two waves a SIMD without spilled registers.
+constexpr int pr_tiles(int dp) { return dp == 256 ? 1 : 2; }
+
+template <typename Tv, int DP, int W>
+__global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
+  constexpr int kMT = pr_tiles(DP), BM = 16 * kMT * W, BN = pr_keys(sizeof(Tv), DP);
+  using C = PrCore<Tv, DP, kMT, W, BN>;
+  constexpr int KT = C::KT, DT = C::DT, QR = C::QR;
+  __shared__ __attribute__((aligned(16))) char lds[4 * C::kTile];
+  __shared__ int s_up[DP], s_down[DP];
+  PrJob j;
+  if (!pr_find<Tv, BM, BN>(a, j)) return;
+  const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  for (int d = threadIdx.x; d < DP; d += 64 * W) s_up[d] = s_down[d] = 0x7fffffff;
+  uint32_t off_k[C::PIECES], off_v[C::PIECES];
+  C::offsets(off_k, off_v, wave, a);
+  auto load = [&](int buf, int key) {
+    C::load(lds + buf * 2 * C::kTile, j.k, a.k_stride, key, j.hi, a.D, off_k, wave);
+    C::load(lds + buf * 2 * C::kTile + C::kTile, j.v, a.v_stride, key, j.hi, a.D, off_v, wave);
+  };
+  if (j.lo < j.hi) load(0, j.lo);
+  const int w_m = j.m0 + wave * 16 * kMT;        // the wave's first column
+  int last[kMT];                                 // of a column: its last key
+  u32x4_t q[kMT][QR];
+#pragma unroll
+  for (int i = 0; i < kMT; ++i) {
+    const int m = w_m + 16 * i + r, tok = m / a.nq;
+    const bool in = m < j.cols;
+    last[i] = in ? j.past + tok : -1;
+    const Tv* const row = static_cast<const Tv*>(a.q) +
+                          (in ? (j.row0 + tok) * a.q_stride +
+                                (int64_t)(j.h * a.nq + m % a.nq) * a.D : 0);
+#pragma unroll
+    for (int t = 0; t < QR; ++t) {
+      const int d = (4 * t + q4) * C::VE;
+      q[i][t] = u32x4_t{0, 0, 0, 0};
+      if (in && d < a.D) q[i][t] = (*reinterpret_cast<const u32x4_t*>(row + d) & a.keep) ^ a.flip;
+    }
+  }
+  // keys of the wave: none from w_hi on, all visible to all of its columns before w_all
+  const int w_end = min(w_m + 16 * kMT, j.cols);
+  const int w_hi = w_m < j.cols ? min(j.hi, j.past + (w_end - 1) / a.nq + 1) : 0;
+  const int w_all = w_end - w_m == 16 * kMT ? j.past + w_m / a.nq + 1 : 0;
+  // before which key no column of the block needs a mask
+  const int b_all = j.m0 + BM <= j.cols ? j.past + j.m0 / a.nq + 1 : 0;
+
+  f32x4_t o[kMT][DT];
+  float m_run[kMT], l_run[kMT];
+#pragma unroll
+  for (int i = 0; i < kMT; ++i) {
+    m_run[i] = -INFINITY;
+    l_run[i] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[i][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
   __syncthreads();
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int64_t j0 = 0; j0 < keys; j0 += kThreads) {
-    float s = -INFINITY;
-    if (j0 + t < keys) {
-      s = 0.f;
-      for (int d = 0; d < a.D; ++d) s = fmaf(s_q[d], as_f32(k[(j0 + t) * a.k_stride + d]), s);
-      s *= a.scale2;
+  int buf = 0;
+  for (int key = j.lo; key < j.hi; key += BN, buf ^= 1) {
+    char* const tk = lds + buf * 2 * C::kTile;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down);
+    // the tile has landed, and every wave is done with the other buffer
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (key + BN < j.hi) load(buf ^ 1, key + BN);
+    if (key >= w_hi) continue;
+    f32x4_t s[kMT][KT];
+    C::scores(s, q, tk);
+    if (key + BN > w_all) {
+#pragma unroll
+      for (int i = 0; i < kMT; ++i)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key + 16 * kt + 4 * q4 + e > last[i]) s[i][kt][e] = -INFINITY;
     }
-    float top = s;
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
-    if (lane_id() == 0) s_red[t / kWave] = top;
-    __syncthreads();
-    for (int w = 0; w < kThreads / kWave; ++w) top = fmaxf(top, s_red[w]);
-    top = fmaxf(top, m);
-    const float mu = top == -INFINITY ? 0.f : top, f = exp2f(m - mu);
-    const float p = j0 + t < keys ? exp2f(s - mu) : 0.f;
-    s_p[t] = p;
-    float sum = wave_sum(p);
-    __syncthreads();
-    if (lane_id() == 0) s_red[t / kWave] = sum;
-    __syncthreads();
-    l *= f;
-    o *= f;
-    m = top;
-    for (int w = 0; w < kThreads / kWave; ++w) l += s_red[w];
-    if (t < a.D) {
-      const int64_t c = min((int64_t)kThreads, keys - j0);
-      for (int64_t j = 0; j < c; ++j) o = fmaf(s_p[j], as_f32(v[(j0 + j) * a.v_stride + t]), o);
-    }
-    __syncthreads();
+    softmax_step(s, m_run, l_run, o, a.scale2);
+    C::values(o, s, tk + C::kTile);
   }
-  const int64_t at = n * a.Hq + h;
-  if (t < a.D) put(static_cast<Tv*>(a.out) + at * a.D + t, l == 0.f ? 0.f : o / l);
-  if (a.lse && t == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  __syncthreads();
+  const int64_t RH = a.N * a.Hq;
+#pragma unroll
+  for (int i = 0; i < kMT; ++i) {
+    const float l = quad_sum(l_run[i]);
+    const int m = w_m + 16 * i + r;
+    if (m >= j.cols) continue;
+    const int64_t to = j.split * RH + (j.row0 + m / a.nq) * a.Hq + j.h * a.nq + m % a.nq;
+    const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    if (q4 == 0) {
+      if (a.splits > 1) a.part_ml[to] = make_float2(m_run[i], l);
+      else if (a.lse) a.lse[to] = lse_of(m_run[i], l);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int d = 16 * dt + 4 * q4;            // D is a multiple of 8
+      if (d >= a.D) continue;
+      f32x4_t x = o[i][dt] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (last[i] >= s_up[d + e]) x[e] += INFINITY;
+        if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
+      }
+      if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part_o + to * a.D + d) = x;
+      else put4(static_cast<Tv*>(a.out) + to * a.D + d, x);
+    }
+  }
+}
+
+struct PrPlan {
+  int dp, waves, splits;
+  int64_t slots, blocks;
+  size_t ml, total;
+};
+
+constexpr int kWant = 256;                       // blocks that fill the card
+
+// Few row tiles: keys are split over blocks. With b blocks a split, ceil(kWant / b)
+// splits of N Hq rows, b at least N Hq / BM, are at most N Hq + kWant BM rows, and more
+// than one split has at most kWant BM of them: `total` allows every call for as many
+// as any of fewer tokens, keys or sequences has.
+PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
+  PrPlan pl{};
+  const int nq = Hq / Hkv;
+  pl.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  pl.waves = 8;
+  const int64_t bm = 16 * pr_tiles(pl.dp) * pl.waves, RH = N * Hq;
+  pl.slots = N * nq / bm + B;
+  auto most = [](int64_t keys) { return std::min<int64_t>(std::max<int64_t>(1, keys / 512), 64); };
+  const int64_t used = ceil_div(N * nq, bm) * Hkv;
+  pl.splits = (int)std::min(most(ceil_div(M, B)), ceil_div(kWant, used));
+  pl.blocks = pl.slots * Hkv * pl.splits;
+  const int64_t rows = most(M) == 1 ? 0
+                                    : std::min(RH * most(M), std::min(RH, kWant * bm) + kWant * bm);
+  pl.ml = align_up((size_t)rows * D * 4, 256);
+  pl.total = align_up(pl.ml + (size_t)rows * 8, 256);
+  return pl;
 }
 
 bool pr_ok(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
@@ -103,12 +411,32 @@ bool pr_supported(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int3
          (int64_t)Hq * D <= (1 << 24) && N * Hq / 32 + (double)B * Hkv < (1 << 22);
 }
 
+template <typename Tv, int DP>
+int pr_launch(const PrArgs& a, const PrPlan& pl, hipStream_t st) {
+  pr_kernel<Tv, DP, 8><<<dim3((unsigned)pl.blocks), dim3(64 * 8), 0, st>>>(a);
+  MOE_CHECK_LAUNCH();
+  return MOE_OK;
+}
+
+template <typename Tv>
+int pr_run(const PrArgs& a, const PrPlan& pl, hipStream_t st) {
+  const int rc = pl.dp == 64 ? pr_launch<Tv, 64>(a, pl, st)
+               : pl.dp == 128 ? pr_launch<Tv, 128>(a, pl, st)
+                              : pr_launch<Tv, 256>(a, pl, st);
+  if (rc != MOE_OK || a.splits == 1) return rc;
+  const JoinArgs jn = {a.part_o, a.part_ml, a.q_offsets, a.B + 1, a.N * a.Hq, a.Hq, a.D, a.splits,
+                       a.out, a.lse};
+  return attention_join<Tv>(jn, st);
+}
+
 }  // namespace
 }  // namespace moe
 
 extern "C" size_t moe_prompt_attention_workspace(int64_t N, int64_t M, int64_t B, int32_t Hq,
                                                  int32_t Hkv, int32_t D, int32_t dtype) {
-  return 0;
+  using namespace moe;
+  if (!pr_ok(N, M, B, Hq, Hkv, D, dtype) || !pr_supported(N, M, B, Hq, Hkv, D)) return 0;
+  return pr_plan(N, M, B, Hq, Hkv, D, dtype).total;
 }
 
 extern "C" int moe_prompt_attention(const void* q, const void* k, const void* v, int32_t dtype,
@@ -131,12 +459,18 @@ extern "C" int moe_prompt_attention(const void* q, const void* k, const void* v,
   uintptr_t bits = 0;
   for (const void* p : {q, k, v, static_cast<const void*>(out)}) bits |= reinterpret_cast<uintptr_t>(p);
   if (bits & 15) return MOE_ERR_UNSUPPORTED;     // 16-byte loads
+  const PrPlan pl = pr_plan(N, M, B, Hq, Hkv, D, dtype);
   const Span in[] = {span_rows(q, N, q_stride * elt, Hq * D * elt),
                      span_rows(k, M, k_stride * elt, Hkv * D * elt),
                      span_rows(v, M, v_stride * elt, Hkv * D * elt),
                      {q_offsets, (B + 1) * 4}, {k_offsets, (B + 1) * 4}};
-  const Span outs[] = {{out, N * Hq * D * elt}, {lse, N * Hq * 4}};
+  const Span outs[] = {{out, N * Hq * D * elt}, {lse, N * Hq * 4},
+                       {workspace, pl.splits > 1 ? (int64_t)pl.total : 0}};
   MOE_CHECK_ARG(spans_apart(outs, in));
+  if (pl.splits > 1 &&
+      (!workspace || ws_bytes < pl.total || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return MOE_ERR_WORKSPACE;
+  const ScoreScale sc = score_scale(scale, dtype == MOE_BF16);
   PrArgs a{};
   a.q = q;
   a.k = k;
@@ -152,13 +486,16 @@ extern "C" int moe_prompt_attention(const void* q, const void* k, const void* v,
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.D = D;
-  a.scale2 = scale * kLog2e;
+  a.nq = Hq / Hkv;
+  a.scale2 = sc.scale2;
+  a.keep = sc.keep;
+  a.flip = sc.flip;
+  a.splits = pl.splits;
+  a.slots = pl.slots;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.ml);
   a.out = out;
   a.lse = lse;
-  const dim3 grid((unsigned)(N * Hq));
   hipStream_t st = as_stream(stream);
-  if (dtype == MOE_BF16) pr_simple_kernel<uint16_t><<<grid, dim3(kThreads), 0, st>>>(a);
-  else pr_simple_kernel<float><<<grid, dim3(kThreads), 0, st>>>(a);
-  MOE_CHECK_LAUNCH();
-  return MOE_OK;
+  return dtype == MOE_BF16 ? pr_run<uint16_t>(a, pl, st) : pr_run<float>(a, pl, st);
 }
