@@ -108,6 +108,8 @@ struct JoinArgs {
 
 constexpr int kJoinThreads = 256;
 
+namespace {                                      // a kernel of its own for every source
+
 // tpr threads (at least D / 4) take four dimensions each of a row and head, sg groups
 // of them share the splits (both powers of two).
 template <typename Tv>
@@ -164,5 +166,7 @@ int attention_join(const JoinArgs& a, hipStream_t st) {
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
+
+}  // namespace
 
 }  // namespace moe

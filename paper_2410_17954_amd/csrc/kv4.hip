@@ -33,18 +33,30 @@ __device__ __forceinline__ int kv4_scale(uint32_t amax) {
   return min(max(e, kMinExp), kMaxExp) + 127;
 }
 
-// Code of y = |x| 2^-e: the magnitudes are 0, 0.5, 1, 1.5, 2, 3, 4, 6, and a tie goes to
-// the even code. In steps of 0.5 below 2, 1 below 4, 2 above, rint's ties are those.
-__device__ __forceinline__ uint32_t kv4_code(float x, float inv) {
-  const float y = fminf(fabsf(x) * inv, 6.f);
-  const float r = y < 2.f ? rintf(2.f * y) : y < 4.f ? 2.f + rintf(y) : 4.f + rintf(0.5f * y);
-  return (uint32_t)r | (__float_as_uint(x) >> 28 & 8u);
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+
+// Codes of eight channels over 2^e: the conversion rounds to the nearest, ties to the even
+// code, and takes what is larger as 6.
+__device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float unit) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], unit, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], unit, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], unit, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], unit, 3);
 }
 
-__device__ __forceinline__ float kv4_value(uint32_t code, float unit) {
-  const uint32_t c = code & 7u;
-  const float m = c < 4 ? 0.5f * c : c == 7 ? 6.f : (float)c - 2.f;
-  return (code & 8u ? -m : m) * unit;
+// The values of eight codes; those of a scale of 255 are NaN.
+__device__ __forceinline__ void kv4_values(uint32_t w, uint32_t scale, float (&x)[8]) {
+  const float unit = __uint_as_float(scale << 23);
+  const f32x2_t v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = v[i][0];
+    x[2 * i + 1] = v[i][1];
+  }
 }
 
 template <typename Tv> struct Eight;
@@ -98,12 +110,7 @@ __global__ void __launch_bounds__(kThreads) kv4_store_kernel(Kv4Args a) {
   top = max(top, (uint32_t)dpp<0xB1>((int)top));
   top = max(top, (uint32_t)dpp<0x4E>((int)top));
   const int s = kv4_scale(top);
-  uint32_t w = 0;
-  if (s != kNaNScale) {
-    const float inv = __uint_as_float((uint32_t)(254 - s) << 23);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w |= kv4_code(x[j], inv) << (4 * j);
-  }
+  const uint32_t w = s == kNaNScale ? 0 : kv4_codes(x, __uint_as_float((uint32_t)s << 23));
   const int64_t to = slot * a.row + c;
   reinterpret_cast<uint32_t*>(second ? a.v_codes : a.k_codes)[to] = w;
   if ((c & 3) == 0) (second ? a.v_scales : a.k_scales)[to >> 2] = (uint8_t)s;
@@ -120,10 +127,8 @@ __global__ void __launch_bounds__(kThreads) kv4_load_kernel(Kv4Args a) {
   const int64_t from = slot * a.row + c;
   const uint32_t w = reinterpret_cast<const uint32_t*>(second ? a.v_codes : a.k_codes)[from];
   const uint32_t s = (second ? a.v_scales : a.k_scales)[from >> 2];
-  const float unit = s == kNaNScale ? NAN : __uint_as_float(s << 23);
   float x[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = kv4_value(w >> (4 * j), unit);
+  kv4_values(w, s, x);
   Eight<Tv>::put(const_cast<Tv*>(static_cast<const Tv*>(second ? a.v : a.k)) +
                      n * (second ? a.v_stride : a.k_stride) + c * 8, x);
 }

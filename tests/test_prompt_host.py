@@ -144,7 +144,7 @@ def test_workspaces_are_needed_and_refused(lib):
             assert _prompt(lib, **few, **bad) == ops.MOE_ERR_WORKSPACE, bad
     need = lib.moe_kv4_attention_workspace(4, 1000, 8, 2, 64)
     if need:
-        for bad in (dict(ws=None), dict(nbytes=need - 1), dict(ws=ctypes.c_void_p((9 << 44) + 16))):
+        for bad in (dict(ws=None), dict(nbytes=need - 1), dict(ws=ctypes.c_void_p((10 << 44) + 16))):
             assert _attend(lib, **bad) == ops.MOE_ERR_WORKSPACE, bad
         assert _attend(lib, out=at(9)) == ops.MOE_ERR_ARG
     need = lib.moe_token_logprobs_workspace(3, 100000, 2, 4)
