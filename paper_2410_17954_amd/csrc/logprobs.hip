@@ -8,9 +8,10 @@
 // raised only where a logit exceeds it by more than kSlack, so almost never after the
 // first ones.
 // Best alternatives need no second pass over the row: of kGroups groups of threads the
-// n-th largest of their maxima is a bound T that n logits reach, and only threads whose
-// own maximum reaches T hold more of them, about n. A wave reads such a thread's logits
-// again, a lane each 16 bytes, and those from T on are ranked by counting.
+// n-th largest of their maxima, cut to some leading bits, is a bound T that n logits
+// reach, and only threads whose own maximum reaches T hold more of them, about n. A
+// wave reads such a thread's logits again, a lane each 16 bytes, and those from T on
+// are ranked by counting.
 #include "moeflow_prompt.h"
 #include "common.h"
 #include "rows.h"
@@ -27,11 +28,13 @@ namespace {
 constexpr int kMaxTop = 64;
 constexpr int kGroups = 256;
 constexpr int kKeys = 1024;                      // logits from T on that are ranked
+constexpr int kBoundBits = 20;
 constexpr float kSlack = 8.f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // 16 bytes from an address that is only element-aligned.
 struct __attribute__((packed, aligned(2))) Bytes16 { uint32_t w[4]; };
+typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename Tv> struct LpVec;
 template <> struct LpVec<uint16_t> {
@@ -70,38 +73,63 @@ struct LpSum {
   double s, h;
 };
 
+// e^d, d <= 0: the power of two in whole steps apart from the float32 exponential of the
+// rest, so that it is off by an ulp of float32 however small it is; 0 far below.
+__device__ __forceinline__ double lp_exp(double d) {
+  const double x = fmax(d * 1.4426950408889634, -1100.0), n = rint(x);
+  return ldexp((double)__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
+}
+
+// ln x of a positive number, off by 2^-24 (|ln of its mantissa| is below 0.7); NaN of NaN.
+__device__ __forceinline__ double lp_log(double x) {
+  int e;
+  const float f = (float)frexp(x, &e);
+  return (double)e * 0.6931471805599453 + (double)(__builtin_amdgcn_logf(f) * 0.6931471805599453f);
+}
+
 // Brings sums to a reference at least as large. No logits: ref -inf, sums 0.
 __device__ __forceinline__ void lp_raise(LpSum& x, float to) {
-  if (x.ref == to || x.ref == -INFINITY) {
-    x.ref = to;
-    return;
+  if (x.ref != to && x.ref != -INFINITY) {
+    const double d = (double)x.ref - (double)to, f = lp_exp(d);
+    // a factor that underflows leaves nothing, whatever the difference
+    x.h = f > 0.0 || x.s != x.s ? f * (x.h + d * x.s) : 0.0;
+    x.s *= f;
   }
-  const double d = (double)x.ref - (double)to, f = exp(d);
-  // a factor that underflows leaves nothing, whatever the difference
-  x.h = f > 0.0 || x.s != x.s ? f * (x.h + d * x.s) : 0.0;
-  x.s *= f;
   x.ref = to;
 }
 
-template <typename Tv, int T>
+// T threads, U 16-byte loads of each in flight beside the ones in work.
+template <typename Tv, int T, int U, bool NT>
 __global__ void __launch_bounds__(T)
 lp_kernel(LpArgs a) {
   using LV = LpVec<Tv>;
-  constexpr int VE = LV::N, W = T / kWave, U = 4;
+  constexpr int VE = LV::N, W = T / kWave;
+  static_assert(U * VE % 32 == 0 || 32 % (U * VE) == 0, "float32 sums of at most 32 logits");
+  constexpr int PART = U * VE < 32 ? U * VE : 32;
   __shared__ float s_ref[W];
   __shared__ double s_s[W], s_h[W];
-  __shared__ __attribute__((aligned(16))) float s_max[kGroups];
-  __shared__ float s_thr, s_M;
-  __shared__ double s_lnS;
-  __shared__ int s_owners, s_count;
-  __shared__ int16_t s_owner[T];
+  __shared__ float s_max[kGroups];
+  __shared__ int s_count;
   __shared__ float s_key[kKeys];
   __shared__ int32_t s_idx[kKeys];
   const int64_t row = blockIdx.x;
   const Tv* const z = static_cast<const Tv*>(a.logits) + row * a.stride;
-  const int t = threadIdx.x, lane = lane_id(), wave = t / kWave;
+  const int t = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(t / kWave);
   const int V = (int)a.V, nvec = V / VE, rest = V - nvec * VE;
 
+  Bytes16 raw[U];
+  auto load = [&](int at) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at + u * T < nvec) {
+        const Bytes16* const from = reinterpret_cast<const Bytes16*>(z + (int64_t)(at + u * T) * VE);
+        if constexpr (NT) raw[u] = __builtin_bit_cast(Bytes16, __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4_any_t*>(from)));
+        else raw[u] = *from;
+      }
+  };
+  load(t);
   // given tokens: their logits are on the way while the row is
   int32_t tok = -1;
   float ztok = 0.f;
@@ -109,6 +137,7 @@ lp_kernel(LpArgs a) {
     tok = a.tokens[row * a.m + t];
     if (tok >= 0 && tok < V) ztok = LV::one(z + tok);
   }
+  if (t == 0) s_count = 0;
 
   LpSum x = {-INFINITY, 0.0, 0.0};
   float best = -INFINITY;                        // a NaN is no maximum
@@ -129,32 +158,28 @@ lp_kernel(LpArgs a) {
     x.s += (double)s;
     x.h += (double)h;
   };
-  Bytes16 raw[U];
-  auto load = [&](int at) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (at + u * T < nvec) raw[u] = *reinterpret_cast<const Bytes16*>(z + (int64_t)(at + u * T) * VE);
-  };
-  load(t);
   for (int at = t; at < nvec; at += U * T) {
-    float v[U][VE];
+    float v[U * VE];
 #pragma unroll
-    for (int u = 0; u < U; ++u) LV::unpack(raw[u], v[u]);
-    if (at + U * T < nvec) load(at + U * T);
-    if (at + (U - 1) * T < nvec) {
-      add(&v[0][0], U * VE);
-    } else {
+    for (int u = 0; u < U; ++u) LV::unpack(raw[u], v + u * VE);
+    const bool whole = at + (U - 1) * T < nvec;
+    if (!whole) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (at + u * T < nvec) add(v[u], VE);
+      for (int u = 1; u < U; ++u)
+        if (at + u * T >= nvec)
+#pragma unroll
+          for (int i = 0; i < VE; ++i) v[u * VE + i] = -INFINITY;
     }
+    if (at + U * T < nvec) load(at + U * T);
+#pragma unroll
+    for (int i = 0; i < U * VE; i += PART) add(v + i, PART);
   }
   if (t < rest) {
     const float v = LV::one(z + nvec * VE + t);
     add(&v, 1);
   }
 
-  // the block's sums
+  // the waves' sums and the groups' maxima
   float ref = x.ref;
   for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, kWave));
   lp_raise(x, ref);
@@ -165,46 +190,34 @@ lp_kernel(LpArgs a) {
     s_s[wave] = x.s;
     s_h[wave] = x.h;
   }
-  float gmax = best;
-  if (T > kGroups) {                             // a group is T / kGroups neighbours
-    gmax = fmaxf(gmax, dpp<0xB1>(gmax));
-    if (T == 4 * kGroups) gmax = fmaxf(gmax, dpp<0x4E>(gmax));
-  }
+  float gmax = best;                             // a group is T / kGroups neighbours
+  if (T > kGroups) gmax = fmaxf(gmax, dpp<0xB1>(gmax));
+  if (T > 2 * kGroups) gmax = fmaxf(gmax, dpp<0x4E>(gmax));
   if (t % (T / kGroups) == 0) s_max[t / (T / kGroups)] = gmax;
-  if (t == 0) s_owners = s_count = 0;
   __syncthreads();
-  if (t == 0) {
-    float M = s_ref[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w) M = fmaxf(M, s_ref[w]);
-    double S = 0.0, H = 0.0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      LpSum y = {s_ref[w], s_s[w], s_h[w]};
-      lp_raise(y, M);
-      S += y.s;
-      H += y.h;
-    }
-    const bool none = M == -INFINITY && S == 0.0;
-    const double lnS = none ? 0.0 : log(S);
-    if (a.entropy) a.entropy[row] = none ? 0.f : (float)(lnS - H / S);
-    s_M = none ? 0.f : M;
-    s_lnS = lnS;                                 // NaN of a row with a NaN or +inf
-  }
-  if (a.n_top > 0 && t < kGroups) {              // the n-th largest of the groups' maxima
-    const float mine = s_max[t];
-    int r = 0;
-    for (int i = 0; i < kGroups; i += 4) {
-      const f32x4_t o = *reinterpret_cast<const f32x4_t*>(s_max + i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) r += o[e] > mine || (o[e] == mine && i + e < t);
-    }
-    if (r == a.n_top - 1) s_thr = fmaxf(mine, -FLT_MAX);     // -inf is no candidate
-  }
-  __syncthreads();
-  const float M = s_M;
-  const double lnS = s_lnS;
-  const bool bad = lnS != lnS;
+
+  // the row's: every wave for itself, lane w % 16 the sums of wave w
+  float M = s_ref[lane % 16 % W];
+  LpSum y = {M, s_s[lane % 16 % W], s_h[lane % 16 % W]};
+  if (lane % 16 >= W) y.s = y.h = 0.0;
+  M = fmaxf(M, dpp<0xB1>(M));
+  M = fmaxf(M, dpp<0x4E>(M));
+  M = fmaxf(M, dpp<0x141>(M));
+  M = fmaxf(M, dpp<0x140>(M));
+  lp_raise(y, M);
+  double S = y.s, H = y.h;
+  auto row_sum = [](double v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    return v + dpp<0x140>(v);
+  };
+  S = row_sum(S);
+  H = row_sum(H);
+  const bool none = M == -INFINITY && S == 0.0;
+  const double lnS = none ? 0.0 : lp_log(S);     // NaN of a row with a NaN or +inf
+  if (none) M = 0.f;
+  if (t == 0 && a.entropy) a.entropy[row] = none ? 0.f : (float)(lnS - H / S);
   // the difference to the maximum first: beside a mask's lowest number ln S is lost
   auto logprob = [&](float v) { return (float)((double)v - (double)M - lnS); };
   for (int64_t j = t; j < a.m; j += T) {
@@ -217,34 +230,47 @@ lp_kernel(LpArgs a) {
   if (a.n_top == 0) return;
   int32_t* const out_idx = a.top_tokens + row * a.n_top;
   float* const out_val = a.top_logprobs + row * a.n_top;
-  if (bad) {
+  if (lnS != lnS) {
     for (int j = t; j < a.n_top; j += T) {
       out_idx[j] = -1;
       out_val[j] = -INFINITY;
     }
     return;
   }
-  const float thr = s_thr;
-  if (best >= thr) s_owner[atomicAdd(&s_owners, 1)] = (int16_t)t;
-  __syncthreads();
-  const int owners = s_owners;
+  // T: the largest number of kBoundBits leading bits that n_top groups reach, bit by bit
+  // over the maxima's order; not below the lowest number, -inf is no candidate
+  uint32_t key[kGroups / kWave], bound = 0;
+#pragma unroll
+  for (int i = 0; i < kGroups / kWave; ++i) key[i] = float_order(s_max[i * kWave + lane]);
+  for (int bit = 31; bit > 31 - kBoundBits; --bit) {
+    const uint32_t to = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kGroups / kWave; ++i) n += (int)__popcll(ballot(key[i] >= to));
+    if (n >= a.n_top) bound = to;
+  }
+  bound = max(bound, float_order(-FLT_MAX));
   auto offer = [&](float v, int i) {
-    if (!(v >= thr)) return;
     const int at = atomicAdd(&s_count, 1);
     if (at < kKeys) {
       s_key[at] = v;
       s_idx[at] = i;
     }
   };
-  for (int o = wave; o < owners; o += W) {
-    const int own = s_owner[o];
-    for (int at = own + lane * T; at < nvec; at += kWave * T) {
+  // a wave reads again what its threads of a maximum from T on had read
+  for (uint64_t own = ballot(float_order(best) >= bound); own; own &= own - 1) {
+    const int o = wave * kWave + __ffsll((unsigned long long)own) - 1;
+    for (int at = o + lane * T; at < nvec; at += kWave * T) {
       float v[VE];
       LV::unpack(*reinterpret_cast<const Bytes16*>(z + (int64_t)at * VE), v);
 #pragma unroll
-      for (int i = 0; i < VE; ++i) offer(v[i], at * VE + i);
+      for (int i = 0; i < VE; ++i)
+        if (float_order(v[i]) >= bound) offer(v[i], at * VE + i);
     }
-    if (lane == 0 && own < rest) offer(LV::one(z + nvec * VE + own), nvec * VE + own);
+    if (lane == 0 && o < rest) {
+      const float v = LV::one(z + nvec * VE + o);
+      if (float_order(v) >= bound) offer(v, nvec * VE + o);
+    }
   }
   __syncthreads();
   const int count = s_count;
@@ -253,7 +279,9 @@ lp_kernel(LpArgs a) {
       const float v = s_key[i];
       const int32_t id = s_idx[i];
       int r = 0;
-      for (int o = 0; o < count; ++o) r += s_key[o] > v || (s_key[o] == v && s_idx[o] < id);
+#pragma unroll 4
+      for (int o = 0; o < count; ++o)
+        r += (s_key[o] > v) | ((s_key[o] == v) & (s_idx[o] < id));
       if (r < a.n_top) {
         out_idx[r] = id;
         out_val[r] = logprob(v);
@@ -265,6 +293,7 @@ lp_kernel(LpArgs a) {
     }
     return;
   }
+  __syncthreads();                               // s_key is rewritten below
   // so many equal ones: the best after the one before, again and again over the row
   float pv = INFINITY;
   int pi = -1;
@@ -317,10 +346,16 @@ bool lp_supported(int64_t R, int64_t V, int64_t m, int32_t n_top) {
   return n_top <= kMaxTop && V <= (1 << 24) && R < (1 << 22) && m < ((int64_t)1 << 31) / R;
 }
 
+// Rows that the compute units hold at once go to blocks of 1024 threads, which have more
+// of a row in flight (one row of 128000 bf16 logits 11 us without alternatives, with 256
+// threads 29); more rows to blocks of 256, eight a compute unit (300 rows of 32000: 8.2
+// us, of 1024 threads 13.7), whose logits are more than the caches keep, so that the
+// non-temporal hint pays (2000 rows of 128000: 97 us, 5.3 TB/s, without it 106; 64 rows,
+// which the caches hold, 13.4 with it, 11.6 without).
 template <typename Tv>
 int lp_run(const LpArgs& a, int64_t R, hipStream_t st) {
-  if (R <= 256) lp_kernel<Tv, 1024><<<dim3((unsigned)R), dim3(1024), 0, st>>>(a);
-  else lp_kernel<Tv, 256><<<dim3((unsigned)R), dim3(256), 0, st>>>(a);
+  if (R <= 256) lp_kernel<Tv, 1024, 8, false><<<dim3((unsigned)R), dim3(1024), 0, st>>>(a);
+  else lp_kernel<Tv, 256, 4, true><<<dim3((unsigned)R), dim3(256), 0, st>>>(a);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
