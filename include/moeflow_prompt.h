@@ -118,7 +118,7 @@ int moe_kv4_load(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t*
  * workspace  moe_kv4_attention_workspace bytes, 256-byte aligned; a size that does
  *            not fall as R or S grows: that of the largest call serves all
  * Limits: R, C, S >= 1, Hq a multiple of Hkv, D a multiple of 32 up to 256; R * Hq,
- *   C, S < 2^31, Hkv * D < 2^24, q, out and codes on 16 bytes,
+ *   C, S < 2^31, Hkv * D < 2^24, q, out and codes on 16 bytes, scales on 4,
  *   R * Hkv * ceil(Hq / Hkv / 16) below 2^22, |scale| as for moe_prompt_attention.
  *   Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */

@@ -106,65 +106,86 @@ struct JoinArgs {
   float* lse;
 };
 
-constexpr int kJoinThreads = 256;
-
 namespace {                                      // a kernel of its own for every source
 
-// tpr threads (at least D / 4) take four dimensions each of a row and head, sg groups
-// of them share the splits (both powers of two).
-template <typename Tv>
-__global__ void __launch_bounds__(kJoinThreads)
+// Block of T threads: tpr of them (at least D / 4) take four dimensions each of a row
+// and head, the T / rows_per_block / tpr groups of them share the splits; all powers of
+// two. Groups are added up in a tree: a fixed order. These launches are latency, so a
+// thread's loads do not wait for each other: the maximum over all splits comes first.
+template <typename Tv, int T>
+__global__ void __launch_bounds__(T)
 attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
-  __shared__ f32x4_t s_o[kJoinThreads];
-  __shared__ float2 s_ml[kJoinThreads];
+  __shared__ f32x4_t s_o[T];
+  __shared__ float s_l[T], s_m[T];
   const int tpr = 1 << tpr_shift, sg = 1 << sg_shift;
-  const int64_t at = (int64_t)blockIdx.x * (kJoinThreads >> (tpr_shift + sg_shift)) +
+  const int64_t at = (int64_t)blockIdx.x * (T >> (tpr_shift + sg_shift)) +
                      (threadIdx.x >> (tpr_shift + sg_shift));
-  const int d = 4 * (threadIdx.x & (tpr - 1)), g = (threadIdx.x >> tpr_shift) & (sg - 1);
+  const int x = threadIdx.x & (tpr - 1), d = 4 * x, g = (threadIdx.x >> tpr_shift) & (sg - 1);
   const int64_t row = at / a.heads;
   bool live = at < a.RH;
   if (a.offsets) live = live && row >= a.offsets[0] && row < a.offsets[a.n_off - 1];
-  float m = -INFINITY, l = 0.f;
+  const bool mine = live && d < a.D;
+  // maximum over the splits: the threads of a row and head share them all
+  float m = -INFINITY;
+  if (live)
+    for (int p = g * tpr + x; p < a.splits; p += sg * tpr) m = fmaxf(m, a.part_ml[p * a.RH + at].x);
+  const int first = threadIdx.x & ~((tpr << sg_shift) - 1);
+  s_m[threadIdx.x] = m;
+  __syncthreads();
+  for (int n = tpr << sg_shift >> 1; n > 0; n >>= 1) {
+    if ((int)threadIdx.x - first < n) s_m[threadIdx.x] = fmaxf(s_m[threadIdx.x], s_m[threadIdx.x + n]);
+    __syncthreads();
+  }
+  m = s_m[first];
+  const float mu = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-  auto add = [&](const float2 ml, const f32x4_t po) {
-    if (ml.y == 0.f) return;                     // a split without keys wrote no O
-    const float top = fmaxf(m, ml.x), mu = top == -INFINITY ? 0.f : top;
-    const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
-    l = l * f0 + ml.y * f1;
-    o = o * f0 + po * f1;
-    m = top;
-  };
-  if (live && d < a.D) {
+  if (mine) {
 #pragma unroll 4
     for (int p = g; p < a.splits; p += sg) {
       const float2 ml = a.part_ml[p * a.RH + at];
-      add(ml, *reinterpret_cast<const f32x4_t*>(a.part_o + (p * a.RH + at) * a.D + d));
+      f32x4_t po = *reinterpret_cast<const f32x4_t*>(a.part_o + (p * a.RH + at) * a.D + d);
+      float f = __builtin_amdgcn_exp2f(ml.x - mu);
+      if (ml.y == 0.f) {                         // a split without keys wrote no O
+        f = 0.f;
+        po = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      }
+      l = fmaf(ml.y, f, l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(po[e], f, o[e]);
     }
   }
-  if (sg > 1) {
+  for (int n = sg >> 1; n > 0; n >>= 1) {
     s_o[threadIdx.x] = o;
-    s_ml[threadIdx.x] = make_float2(m, l);
+    s_l[threadIdx.x] = l;
     __syncthreads();
-    if (g != 0) return;
-    for (int i = 1; i < sg; ++i)                 // in split group order
-      add(s_ml[threadIdx.x + (i << tpr_shift)], s_o[threadIdx.x + (i << tpr_shift)]);
+    if (g < n) {
+      o += s_o[threadIdx.x + (n << tpr_shift)];
+      l += s_l[threadIdx.x + (n << tpr_shift)];
+    }
+    __syncthreads();
   }
-  if (!live || d >= a.D) return;
+  if (g != 0 || !mine) return;
   o *= l == 0.f ? 0.f : 1.f / l;
   put4(static_cast<Tv*>(a.out) + at * a.D + d, o);
   if (a.lse && d == 0) a.lse[at] = lse_of(m, l);
 }
 
-template <typename Tv>
-int attention_join(const JoinArgs& a, hipStream_t st) {
+template <typename Tv, int T>
+int attention_join_with(const JoinArgs& a, hipStream_t st) {
   const int tpr_shift = a.D <= 64 ? 4 : a.D <= 128 ? 5 : 6;
-  int sg_shift = 0;
-  while (sg_shift < 8 - tpr_shift && (2 << sg_shift) <= a.splits) ++sg_shift;
-  const int64_t blocks = ceil_div(a.RH, kJoinThreads >> (tpr_shift + sg_shift));
-  attention_join_kernel<Tv><<<dim3((unsigned)blocks), dim3(kJoinThreads), 0, st>>>(a, tpr_shift,
-                                                                                  sg_shift);
+  int t_shift = 0, sg_shift = 0;
+  while ((1 << t_shift) < T) ++t_shift;
+  while (sg_shift < t_shift - tpr_shift && (2 << sg_shift) <= a.splits) ++sg_shift;
+  const int64_t blocks = ceil_div(a.RH, T >> (tpr_shift + sg_shift));
+  attention_join_kernel<Tv, T><<<dim3((unsigned)blocks), dim3(T), 0, st>>>(a, tpr_shift, sg_shift);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
+}
+
+template <typename Tv>
+int attention_join(const JoinArgs& a, hipStream_t st) {
+  return a.splits > 32 ? attention_join_with<Tv, 1024>(a, st) : attention_join_with<Tv, 256>(a, st);
 }
 
 }  // namespace
