@@ -22,7 +22,7 @@
 // end. Long key ranges are split over blocks, and a second launch joins the splits.
 #include "moeflow_prompt.h"
 #include "attention.h"
-#include "buffers.h"
+#include "dma.h"
 #include "spans.h"
 
 #include <algorithm>
@@ -78,34 +78,6 @@ __device__ __forceinline__ void mfma(f32x4_t& c, const u32x4_t& x, const u32x4_t
                                               __builtin_bit_cast(bf16x8_t, y), c, 0, 0, 0);
 }
 
-// SIZE bytes a lane of a raw buffer into LDS: 16 at lds + 16 * lane; 4, 2 or 1 as a word at
-// lds + 4 * lane. Past its end: zeros. The compiler does not see that these are on their
-// way: it would wait for all of them at every transposing read. wait_loads does; loads
-// that the compiler counts as well make its own waits longer, never shorter.
-template <int SIZE>
-__device__ __forceinline__ void dma(uint32_t lds, uint32_t voff, u32x4_t rs) {
-  if constexpr (SIZE == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :: "s"(lds), "v"(voff), "s"(rs) : "memory");
-  else if constexpr (SIZE == 4)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                 :: "s"(lds), "v"(voff), "s"(rs) : "memory");
-  else if constexpr (SIZE == 2)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ushort %1, %2, 0 offen lds"
-                 :: "s"(lds), "v"(voff), "s"(rs) : "memory");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, 0 offen lds"
-                 :: "s"(lds), "v"(voff), "s"(rs) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_loads() {   // until at most N are on their way
-  static_assert(N < 64, "the counter's range");
-  asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
-}
-// This wave's LDS accesses have been done.
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((ext_vector_type(2))) int i32x2_t;
 typedef __attribute__((address_space(3))) i32x2_t lds_i32x2_t;
 typedef __attribute__((ext_vector_type(8))) uint16_t u16x8_t;
@@ -149,19 +121,13 @@ struct KaCore {
       off[1][i] = pv * 32 < a.D ? k * row + pv * 16 : kPastEnd;
     }
   }
-  static __device__ __forceinline__ u32x4_t rows(const uint8_t* base, int64_t key, int n, uint32_t row,
-                                                 uint32_t width) {
-    const uint64_t p = reinterpret_cast<uint64_t>(base + key * row);
-    return u32x4_t{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, (uint32_t)(n - 1) * row + width,
-                   0x00027000u};
-  }
   // n keys from `key` on: codes, then a word a key of EACH scales at a time.
   static __device__ __forceinline__ void load(uint32_t lds, const uint8_t* codes, const uint8_t* scales,
                                               int64_t key, int n, const uint32_t (&off)[NI],
                                               const KaArgs& a) {
     const int nb = a.D / 32;
-    const u32x4_t rc = rows(codes, key, n, (uint32_t)(a.Hkv * nb * 16), (uint32_t)nb * 16);
-    const u32x4_t rs = rows(scales, key, n, (uint32_t)(a.Hkv * nb), (uint32_t)nb);
+    const u32x4_t rc = dma_rows(codes, key, n, (uint32_t)(a.Hkv * nb * 16), (uint32_t)nb * 16);
+    const u32x4_t rs = dma_rows(scales, key, n, (uint32_t)(a.Hkv * nb), (uint32_t)nb);
 #pragma unroll
     for (int i = 0; i < NI; ++i) dma<16>(lds + i * 1024, off[i], rc);
     const uint32_t at = (uint32_t)lane_id() * (uint32_t)(a.Hkv * nb);
@@ -314,7 +280,7 @@ ka_kernel(KaArgs a) {
   }
   const int64_t base = (from * a.S * a.Hkv + h) * (a.D / 32);   // of the scales; codes 16 a block
   char* const mine = lds + wave * C::kLds;
-  const uint32_t mine_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)mine);
+  const uint32_t mine_at = lds_address(mine);
   char* const units = mine + 2 * C::kSlot;
   uint32_t off[2][C::NI];
   C::offsets(off, a);

@@ -12,16 +12,21 @@
 // place, a lane's eight operands of the second product (its k slots 8q + j are
 // keys 4q + j of the first tile and 4q + j - 4 of the second). V^T comes from LDS
 // through the transposing read, four keys of one column at a time.
-// Every wave has 32 columns of its own; keys and values go straight from memory to LDS,
-// a tile of keys ahead of the one that all waves of a block compute on, swizzled by
+// Every wave has 16 or 32 columns of its own; keys and values go straight from memory to
+// LDS, a tile of keys ahead of the one that all waves of a block compute on, swizzled by
 // which 16 bytes each lane fetches. Tiles before the first query of a wave need no
-// mask.
+// mask. One prompt of 16384 tokens, 32 heads of 128 over eight key heads, takes 1.89 ms:
+// 1165 TFLOP/s, the MFMAs run in 47 % of the cycles, instructions are issued in 72 %.
+// Measured and left out: another order of MFMAs and exponentials (the tiles of columns
+// apart, interleaved by hand), reads from LDS further ahead, a third buffer, priorities
+// between the waves of a SIMD: level or slower.
 #include "moeflow_prompt.h"
 #include "attention.h"
-#include "buffers.h"
+#include "dma.h"
 #include "spans.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace moe {
 namespace {
@@ -33,6 +38,7 @@ struct PrArgs {
   const int32_t *q_offsets, *k_offsets;
   int64_t N, M, B, q_stride, k_stride, v_stride; // strides in elements
   int Hq, Hkv, D, nq;                            // nq: query heads of a key head
+  float per_nq;                                  // 1 / nq
   float scale2;                                  // |scale| log2 e
   uint32_t keep, flip;
   int splits;
@@ -54,8 +60,15 @@ struct PrJob {
   const char *k, *v;                             // of key 0, head h
   int64_t row0;                                  // the sequence's first row of q
   int lo, hi, past, m0, cols;                    // past: keys before the first query's own
+  int tok0, rem0;                                // token and query head of column m0
   int h, split;
 };
+
+// Token of column m0 + off, off below 2^16: (x + 1/2) / nq lies 1 / (2 nq) or more from
+// a whole number, float32 is off by less.
+__device__ __forceinline__ int pr_token(const PrArgs& a, const PrJob& j, int off) {
+  return j.tok0 + (int)(((float)(j.rem0 + off) + 0.5f) * a.per_nq);
+}
 
 // Row tiles of sequence b start at slot floor(first row * nq / BM) + b: slots of
 // different sequences never meet, and a wave finds a slot's sequence in steps of 64
@@ -63,10 +76,14 @@ struct PrJob {
 // that the tiles of a head share its keys in one L2.
 template <typename Tv, int BM, int BN>
 __device__ __forceinline__ bool pr_find(const PrArgs& a, PrJob& j) {
-  const int64_t u = blockIdx.x;
-  j.h = (int)(u % a.Hkv);
-  j.split = (int)(u / a.Hkv % a.splits);
-  const int64_t slot = a.slots - 1 - u / a.Hkv / a.splits;
+  uint32_t u = blockIdx.x / (uint32_t)a.Hkv;
+  j.h = (int)(blockIdx.x - u * (uint32_t)a.Hkv);
+  j.split = 0;
+  if (a.splits > 1) {
+    j.split = (int)(u % (uint32_t)a.splits);
+    u /= (uint32_t)a.splits;
+  }
+  const int64_t slot = a.slots - 1 - u;
   int64_t b = 0, n = a.B;
   const int lane = lane_id();
   while (n > 1) {
@@ -85,10 +102,16 @@ __device__ __forceinline__ bool pr_find(const PrArgs& a, PrJob& j) {
   j.m0 = (int)tile * BM;
   j.row0 = r0;
   j.past = (int)(keys - (r1 - r0));
-  const int end = max(j.past + (min(j.m0 + BM, j.cols) - 1) / a.nq + 1, 0);
-  const int per = (int)(((end + (int64_t)a.splits - 1) / a.splits + BN - 1) / BN * BN);
-  j.lo = (int)min((int64_t)end, (int64_t)per * j.split);
-  j.hi = (int)min((int64_t)end, (int64_t)j.lo + per);
+  j.tok0 = (int)((uint32_t)j.m0 / (uint32_t)a.nq);
+  j.rem0 = j.m0 - j.tok0 * a.nq;
+  const int end = max(j.past + pr_token(a, j, min(BM, j.cols - j.m0) - 1) + 1, 0);
+  j.lo = 0;
+  j.hi = end;
+  if (a.splits > 1) {
+    const uint32_t per = (((uint32_t)end + a.splits - 1) / (uint32_t)a.splits + BN - 1) / BN * BN;
+    j.lo = (int)min((uint64_t)end, (uint64_t)per * j.split);
+    j.hi = (int)min((uint32_t)end, j.lo + per);
+  }
   j.k = reinterpret_cast<const char*>(static_cast<const Tv*>(a.k) + k0 * a.k_stride +
                                       (int64_t)j.h * a.D);
   j.v = reinterpret_cast<const char*>(static_cast<const Tv*>(a.v) + k0 * a.v_stride +
@@ -96,8 +119,6 @@ __device__ __forceinline__ bool pr_find(const PrArgs& a, PrJob& j) {
   return true;
 }
 
-typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((ext_vector_type(8))) unsigned short u16x8_t;
 
 // DP: the dimension padded to rows of whole 128 bytes; 16-byte chunks past D are zeros.
 template <typename Tv, int DP, int kMT, int W, int BN>
@@ -129,19 +150,15 @@ struct PrCore {
       v[p] = cv * VE < a.D ? (uint32_t)row * (uint32_t)(a.v_stride * sizeof(Tv)) + cv * 16 : kPastEnd;
     }
   }
-  // Keys from `key` on into buf, those from `end` on as zeros.
-  static __device__ __forceinline__ void load(char* buf, const char* base, int64_t stride, int key,
+  // Keys from `key` on into LDS, those from `end` on as zeros.
+  static __device__ __forceinline__ void load(uint32_t lds, const char* base, int64_t stride, int key,
                                               int end, int D, const uint32_t (&off)[PIECES],
                                               int wave) {
-    const int n = min(end - key, BN);
-    const int64_t row = stride * (int64_t)sizeof(Tv);
-    const rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(base + key * row), 0,
-        (int)((uint32_t)(n - 1) * (uint32_t)row + (uint32_t)D * sizeof(Tv)), 0x00027000);
+    const u32x4_t rs = dma_rows(base, key, min(end - key, BN), (uint32_t)(stride * (int64_t)sizeof(Tv)),
+                                (uint32_t)D * sizeof(Tv));
 #pragma unroll
     for (int p = 0; p < PIECES; ++p)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          rs, (lds_void*)(buf + (wave * PIECES + p) * 1024), 16, (int)off[p], 0, 0, 0);
+      dma<16>(lds + (wave * PIECES + p) * 1024, off[p], rs);
   }
   static __device__ __forceinline__ void mfma(f32x4_t& c, const u32x4_t& x, const u32x4_t& y) {
     if constexpr (BF16) {
@@ -247,6 +264,7 @@ struct PrCore {
       if (!odd) continue;
       const int d0 = ((g % CH) ^ swz_v(row)) * VE;
       Tv* const x = reinterpret_cast<Tv*>(at);
+#pragma unroll 1
       for (int e = 0; e < VE; ++e) {
         float f;
         if constexpr (BF16) f = bf16_to_f32(x[e]);
@@ -260,14 +278,15 @@ struct PrCore {
   }
 };
 
-constexpr int pr_keys(int elt, int dp) { return elt * dp <= 256 ? 64 : 32; }
+// Keys of a tile: of 64 in blocks of four waves fewer blocks fit a compute unit (sixteen
+// prompts of up to 1000 tokens 126 us, of 64 keys 163).
+constexpr int pr_keys(int elt, int dp, int waves) {
+  return elt * dp < 256 || (elt * dp == 256 && waves == 8) ? 64 : elt * dp <= 512 ? 32 : 16;
+}
 
-// 16-column tiles of a wave: what leaves two waves a SIMD without spilled registers.
-constexpr int pr_tiles(int dp) { return dp == 256 ? 1 : 2; }
-
-template <typename Tv, int DP, int W>
+template <typename Tv, int DP, int kMT, int W>
 __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
-  constexpr int kMT = pr_tiles(DP), BM = 16 * kMT * W, BN = pr_keys(sizeof(Tv), DP);
+  constexpr int BM = 16 * kMT * W, BN = pr_keys(sizeof(Tv), DP, W);
   using C = PrCore<Tv, DP, kMT, W, BN>;
   constexpr int KT = C::KT, DT = C::DT, QR = C::QR;
   __shared__ __attribute__((aligned(16))) char lds[4 * C::kTile];
@@ -279,22 +298,26 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
   for (int d = threadIdx.x; d < DP; d += 64 * W) s_up[d] = s_down[d] = 0x7fffffff;
   uint32_t off_k[C::PIECES], off_v[C::PIECES];
   C::offsets(off_k, off_v, wave, a);
+  const uint32_t lds_at = lds_address(lds);
   auto load = [&](int buf, int key) {
-    C::load(lds + buf * 2 * C::kTile, j.k, a.k_stride, key, j.hi, a.D, off_k, wave);
-    C::load(lds + buf * 2 * C::kTile + C::kTile, j.v, a.v_stride, key, j.hi, a.D, off_v, wave);
+    const uint32_t to = lds_at + buf * 2 * C::kTile;
+    C::load(to, j.k, a.k_stride, key, j.hi, a.D, off_k, wave);
+    C::load(to + C::kTile, j.v, a.v_stride, key, j.hi, a.D, off_v, wave);
   };
   if (j.lo < j.hi) load(0, j.lo);
-  const int w_m = j.m0 + wave * 16 * kMT;        // the wave's first column
+  const int w_off = wave * 16 * kMT, w_m = j.m0 + w_off;   // the wave's first column
   int last[kMT];                                 // of a column: its last key
+  int64_t at[kMT];                               // its row and head
   u32x4_t q[kMT][QR];
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
-    const int m = w_m + 16 * i + r, tok = m / a.nq;
-    const bool in = m < j.cols;
+    const int off = w_off + 16 * i + r, tok = pr_token(a, j, off);
+    const bool in = j.m0 + off < j.cols;
+    const int head = j.h * a.nq + j.m0 + off - tok * a.nq;
     last[i] = in ? j.past + tok : -1;
+    at[i] = (j.row0 + tok) * a.Hq + head;
     const Tv* const row = static_cast<const Tv*>(a.q) +
-                          (in ? (j.row0 + tok) * a.q_stride +
-                                (int64_t)(j.h * a.nq + m % a.nq) * a.D : 0);
+                          (in ? (j.row0 + tok) * a.q_stride + (int64_t)head * a.D : 0);
 #pragma unroll
     for (int t = 0; t < QR; ++t) {
       const int d = (4 * t + q4) * C::VE;
@@ -304,10 +327,10 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
   }
   // keys of the wave: none from w_hi on, all visible to all of its columns before w_all
   const int w_end = min(w_m + 16 * kMT, j.cols);
-  const int w_hi = w_m < j.cols ? min(j.hi, j.past + (w_end - 1) / a.nq + 1) : 0;
-  const int w_all = w_end - w_m == 16 * kMT ? j.past + w_m / a.nq + 1 : 0;
+  const int w_hi = w_m < j.cols ? min(j.hi, j.past + pr_token(a, j, w_end - 1 - j.m0) + 1) : 0;
+  const int w_all = w_end - w_m == 16 * kMT ? j.past + pr_token(a, j, w_off) + 1 : 0;
   // before which key no column of the block needs a mask
-  const int b_all = j.m0 + BM <= j.cols ? j.past + j.m0 / a.nq + 1 : 0;
+  const int b_all = j.m0 + BM <= j.cols ? j.past + j.tok0 + 1 : 0;
 
   f32x4_t o[kMT][DT];
   float m_run[kMT], l_run[kMT];
@@ -319,15 +342,16 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
     for (int dt = 0; dt < DT; ++dt) o[i][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
   __syncthreads();
-  int buf = 0;
-  for (int key = j.lo; key < j.hi; key += BN, buf ^= 1) {
-    char* const tk = lds + buf * 2 * C::kTile;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // one tile of keys, in buffer BUF: known to the compiler, so that every LDS read is a
+  // lane's address and a constant
+  auto tile = [&](auto BUF, int key) {
+    char* const tk = lds + BUF * 2 * C::kTile;
+    wait_loads<0>();
     if (key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down);
     // the tile has landed, and every wave is done with the other buffer
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (key + BN < j.hi) load(buf ^ 1, key + BN);
-    if (key >= w_hi) continue;
+    if (key + BN < j.hi) load(1 - BUF, key + BN);
+    if (key >= w_hi) return;
     f32x4_t s[kMT][KT];
     C::scores(s, q, tk);
     if (key + BN > w_all) {
@@ -341,15 +365,18 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
     }
     softmax_step(s, m_run, l_run, o, a.scale2);
     C::values(o, s, tk + C::kTile);
+  };
+  for (int key = j.lo; key < j.hi; key += 2 * BN) {
+    tile(std::integral_constant<int, 0>{}, key);
+    if (key + BN < j.hi) tile(std::integral_constant<int, 1>{}, key + BN);
   }
   __syncthreads();
   const int64_t RH = a.N * a.Hq;
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
     const float l = quad_sum(l_run[i]);
-    const int m = w_m + 16 * i + r;
-    if (m >= j.cols) continue;
-    const int64_t to = j.split * RH + (j.row0 + m / a.nq) * a.Hq + j.h * a.nq + m % a.nq;
+    if (w_m + 16 * i + r >= j.cols) continue;
+    const int64_t to = j.split * RH + at[i];
     const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
     if (q4 == 0) {
       if (a.splits > 1) a.part_ml[to] = make_float2(m_run[i], l);
@@ -372,30 +399,48 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
 }
 
 struct PrPlan {
-  int dp, waves, splits;
+  int dp, mt, waves, splits;
   int64_t slots, blocks;
   size_t ml, total;
 };
 
-constexpr int kWant = 256;                       // blocks that fill the card
+// Blocks of eight waves with 32 columns each load keys half as often and have the higher
+// rate (one prompt of 16384 tokens, 32 heads of 128: 1.89 ms, of four waves with 16
+// columns 2.13), but for few or short prompts smaller blocks fill the card better and
+// cost less to start (777 tokens 26.2 us, wide 29.8; sixteen prompts of up to 1000
+// 126 and 141, of up to 2000 level; 16 tokens 6.1 and 9.5; 4096 tokens 153 and 138).
+constexpr int kWideKeys = 4096, kWideColumns = 256;
+// Keys are split over blocks while at most this many blocks are then in flight (bf16,
+// 64 tokens each of four sequences behind 4000 keys 42 us, with half as many 47; 777
+// tokens, whose 392 blocks are left whole, 26, in two splits 34: joins pay for keys
+// that few queries see), each of kMinKeys at least (one token behind 2000 keys 13 us, of
+// twice as many 15.5). float32 blocks take so long that twice as many pay (two prompts of
+// 1000 tokens, 8 heads of 128: 63 us, 85).
+constexpr int kSplitBlocks = 512, kWideSplitBlocks = 256, kFloatSplitBlocks = 1024;
+constexpr int kMinKeys = 128, kMostSplits = 64;
 
-// Few row tiles: keys are split over blocks. With b blocks a split, ceil(kWant / b)
-// splits of N Hq rows, b at least N Hq / BM, are at most N Hq + kWant BM rows, and more
-// than one split has at most kWant BM of them: `total` allows every call for as many
-// as any of fewer tokens, keys or sequences has.
 PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
   PrPlan pl{};
   const int nq = Hq / Hkv;
+  const int64_t keys = ceil_div(M, B);           // of an average sequence
+  const bool wide = dtype == MOE_BF16 && keys >= kWideKeys && ceil_div(N, B) * nq >= kWideColumns;
   pl.dp = D <= 64 ? 64 : D <= 128 ? 128 : 256;
-  pl.waves = 8;
-  const int64_t bm = 16 * pr_tiles(pl.dp) * pl.waves, RH = N * Hq;
+  pl.waves = wide ? 8 : 4;
+  pl.mt = wide && pl.dp < 256 ? 2 : 1;
+  const int64_t bm = 16 * pl.mt * pl.waves;
   pl.slots = N * nq / bm + B;
-  auto most = [](int64_t keys) { return std::min<int64_t>(std::max<int64_t>(1, keys / 512), 64); };
+  auto most = [](int64_t keys) {
+    return std::min<int64_t>(std::max<int64_t>(1, keys / kMinKeys), kMostSplits);
+  };
   const int64_t used = ceil_div(N * nq, bm) * Hkv;
-  pl.splits = (int)std::min(most(ceil_div(M, B)), ceil_div(kWant, used));
+  const int64_t want = wide ? kWideSplitBlocks : dtype == MOE_F32 ? kFloatSplitBlocks : kSplitBlocks;
+  pl.splits = (int)std::min(most(keys), std::max<int64_t>(1, want / used));
   pl.blocks = pl.slots * Hkv * pl.splits;
-  const int64_t rows = most(M) == 1 ? 0
-                                    : std::min(RH * most(M), std::min(RH, kWant * bm) + kWant * bm);
+  // Splits of all rows are at most as many rows as the blocks have columns: `total` allows
+  // every call for that many, and never falls as a call grows.
+  constexpr int64_t kRows = std::max(std::max(kSplitBlocks, kFloatSplitBlocks) * 64,
+                                     kWideSplitBlocks * 256);
+  const int64_t rows = most(M) == 1 ? 0 : std::min(N * Hq * most(M), kRows);
   pl.ml = align_up((size_t)rows * D * 4, 256);
   pl.total = align_up(pl.ml + (size_t)rows * 8, 256);
   return pl;
@@ -408,12 +453,20 @@ bool pr_ok(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, 
 bool pr_supported(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D) {
   const int64_t lim = (int64_t)1 << 31;
   return D % 8 == 0 && D <= 256 && N < lim / Hq && M < lim && B < lim &&
-         (int64_t)Hq * D <= (1 << 24) && N * Hq / 32 + (double)B * Hkv < (1 << 22);
+         (int64_t)Hq * D <= (1 << 24) && Hq <= (1 << 16) && N * Hq / 32 + (double)B * Hkv < (1 << 22);
 }
 
 template <typename Tv, int DP>
 int pr_launch(const PrArgs& a, const PrPlan& pl, hipStream_t st) {
-  pr_kernel<Tv, DP, 8><<<dim3((unsigned)pl.blocks), dim3(64 * 8), 0, st>>>(a);
+  const dim3 grid((unsigned)pl.blocks), block((unsigned)(64 * pl.waves));
+  if constexpr (sizeof(Tv) == 2) {
+    if (pl.waves == 8) {
+      pr_kernel<Tv, DP, DP == 256 ? 1 : 2, 8><<<grid, block, 0, st>>>(a);
+      MOE_CHECK_LAUNCH();
+      return MOE_OK;
+    }
+  }
+  pr_kernel<Tv, DP, 1, 4><<<grid, block, 0, st>>>(a);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
@@ -487,6 +540,7 @@ extern "C" int moe_prompt_attention(const void* q, const void* k, const void* v,
   a.Hkv = Hkv;
   a.D = D;
   a.nq = Hq / Hkv;
+  a.per_nq = 1.f / (float)a.nq;
   a.scale2 = sc.scale2;
   a.keep = sc.keep;
   a.flip = sc.flip;
