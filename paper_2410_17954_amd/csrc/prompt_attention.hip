@@ -284,27 +284,35 @@ constexpr int pr_keys(int elt, int dp, int waves) {
   return elt * dp < 256 || (elt * dp == 256 && waves == 8) ? 64 : elt * dp <= 512 ? 32 : 16;
 }
 
-template <typename Tv, int DP, int kMT, int W>
-__global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
+// KS groups of W waves have the same columns and take tiles of keys in turn; they are
+// added up through LDS at the end.
+template <typename Tv, int DP, int kMT, int W, int KS>
+__global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
   constexpr int BM = 16 * kMT * W, BN = pr_keys(sizeof(Tv), DP, W);
   using C = PrCore<Tv, DP, kMT, W, BN>;
   constexpr int KT = C::KT, DT = C::DT, QR = C::QR;
-  __shared__ __attribute__((aligned(16))) char lds[4 * C::kTile];
+  constexpr int kPart = W * kMT * DT * kWave * 16;   // O of a group
+  constexpr int kLds = KS > 1 && KS * kPart > 4 * KS * C::kTile ? KS * kPart : 4 * KS * C::kTile;
+  __shared__ __attribute__((aligned(16))) char lds[kLds];
+  __shared__ float s_m[KS][W * kMT * 16], s_l[KS][W * kMT * 16];
   __shared__ int s_up[DP], s_down[DP];
   PrJob j;
   if (!pr_find<Tv, BM, BN>(a, j)) return;
   const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  for (int d = threadIdx.x; d < DP; d += 64 * W) s_up[d] = s_down[d] = 0x7fffffff;
+  const int any = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wave = any % W, group = any / W;
+  for (int d = threadIdx.x; d < DP; d += 64 * W * KS) s_up[d] = s_down[d] = 0x7fffffff;
   uint32_t off_k[C::PIECES], off_v[C::PIECES];
   C::offsets(off_k, off_v, wave, a);
-  const uint32_t lds_at = lds_address(lds);
+  char* const ring = lds + group * 4 * C::kTile;
+  const uint32_t ring_at = lds_address(ring);
   auto load = [&](int buf, int key) {
-    const uint32_t to = lds_at + buf * 2 * C::kTile;
+    const uint32_t to = ring_at + buf * 2 * C::kTile;
     C::load(to, j.k, a.k_stride, key, j.hi, a.D, off_k, wave);
     C::load(to + C::kTile, j.v, a.v_stride, key, j.hi, a.D, off_v, wave);
   };
-  if (j.lo < j.hi) load(0, j.lo);
+  const int key0 = j.lo + group * BN;            // the group's first tile
+  if (key0 < j.hi) load(0, key0);
   const int w_off = wave * 16 * kMT, w_m = j.m0 + w_off;   // the wave's first column
   int last[kMT];                                 // of a column: its last key
   int64_t at[kMT];                               // its row and head
@@ -345,12 +353,12 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
   // one tile of keys, in buffer BUF: known to the compiler, so that every LDS read is a
   // lane's address and a constant
   auto tile = [&](auto BUF, int key) {
-    char* const tk = lds + BUF * 2 * C::kTile;
+    char* const tk = ring + BUF * 2 * C::kTile;
     wait_loads<0>();
-    if (key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down);
+    if (key < j.hi && key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down);
     // the tile has landed, and every wave is done with the other buffer
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (key + BN < j.hi) load(1 - BUF, key + BN);
+    if (key + KS * BN < j.hi) load(1 - BUF, key + KS * BN);
     if (key >= w_hi) return;
     f32x4_t s[kMT][KT];
     C::scores(s, q, tk);
@@ -366,15 +374,57 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
     softmax_step(s, m_run, l_run, o, a.scale2);
     C::values(o, s, tk + C::kTile);
   };
-  for (int key = j.lo; key < j.hi; key += 2 * BN) {
-    tile(std::integral_constant<int, 0>{}, key);
-    if (key + BN < j.hi) tile(std::integral_constant<int, 1>{}, key + BN);
+  // as many turns for every group: they meet at the barriers
+  for (int key = j.lo; key < j.hi; key += 2 * KS * BN) {
+    tile(std::integral_constant<int, 0>{}, key + group * BN);
+    if (key + KS * BN < j.hi) tile(std::integral_constant<int, 1>{}, key + (KS + group) * BN);
   }
-  __syncthreads();
+  float l_all[kMT];
+#pragma unroll
+  for (int i = 0; i < kMT; ++i) l_all[i] = quad_sum(l_run[i]);
+  if constexpr (KS > 1) {
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+      if (q4 == 0) {
+        s_m[group][w_off + 16 * i + r] = m_run[i];
+        s_l[group][w_off + 16 * i + r] = l_all[i];
+      }
+    __syncthreads();                             // and every wave is done with its tiles
+    f32x4_t* const part = reinterpret_cast<f32x4_t*>(lds);
+#pragma unroll
+    for (int i = 0; i < kMT; ++i) {
+      const int c = w_off + 16 * i + r;
+      float top = s_m[0][c];
+#pragma unroll
+      for (int g = 1; g < KS; ++g) top = fmaxf(top, s_m[g][c]);
+      const float mu = top == -INFINITY ? 0.f : top;
+      const float f = __builtin_amdgcn_exp2f(m_run[i] - mu);
+      l_all[i] = 0.f;
+#pragma unroll
+      for (int g = 0; g < KS; ++g) l_all[i] += s_l[g][c] * __builtin_amdgcn_exp2f(s_m[g][c] - mu);
+      m_run[i] = top;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        o[i][dt] *= f;
+        if (group > 0) part[((any * kMT + i) * DT + dt) * kWave + lane] = o[i][dt];
+      }
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int g = 1; g < KS; ++g)
+          o[i][dt] += part[(((any + g * W) * kMT + i) * DT + dt) * kWave + lane];
+  } else {
+    __syncthreads();
+  }
   const int64_t RH = a.N * a.Hq;
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
-    const float l = quad_sum(l_run[i]);
+    const float l = l_all[i];
     if (w_m + 16 * i + r >= j.cols) continue;
     const int64_t to = j.split * RH + at[i];
     const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
@@ -399,7 +449,7 @@ __global__ void __launch_bounds__(64 * W, 2) pr_kernel(PrArgs a) {
 }
 
 struct PrPlan {
-  int dp, mt, waves, splits;
+  int dp, mt, waves, groups, splits;             // groups: of waves over one block's keys
   int64_t slots, blocks;
   size_t ml, total;
 };
@@ -407,17 +457,22 @@ struct PrPlan {
 // Blocks of eight waves with 32 columns each load keys half as often and have the higher
 // rate (one prompt of 16384 tokens, 32 heads of 128: 1.89 ms, of four waves with 16
 // columns 2.13), but for few or short prompts smaller blocks fill the card better and
-// cost less to start (777 tokens 26.2 us, wide 29.8; sixteen prompts of up to 1000
+// cost less to start (777 tokens 25.3 us, wide 29.8; sixteen prompts of up to 1000
 // 126 and 141, of up to 2000 level; 16 tokens 6.1 and 9.5; 4096 tokens 153 and 138).
 constexpr int kWideKeys = 4096, kWideColumns = 256;
 // Keys are split over blocks while at most this many blocks are then in flight (bf16,
 // 64 tokens each of four sequences behind 4000 keys 42 us, with half as many 47; 777
 // tokens, whose 392 blocks are left whole, 26, in two splits 34: joins pay for keys
 // that few queries see), each of kMinKeys at least (one token behind 2000 keys 13 us, of
-// twice as many 15.5). float32 blocks take so long that twice as many pay (two prompts of
-// 1000 tokens, 8 heads of 128: 63 us, 85).
-constexpr int kSplitBlocks = 512, kWideSplitBlocks = 256, kFloatSplitBlocks = 1024;
+// twice as many 15.5). float32 blocks take so long that more of them pay (two prompts of
+// 1000 tokens, 8 heads of 128: three splits 63 us, two 85).
+constexpr int kSplitBlocks = 512, kWideSplitBlocks = 256, kFloatSplitBlocks = 768;
 constexpr int kMinKeys = 128, kMostSplits = 64;
+// Two groups of waves on a block's columns while blocks do not fill the card and have
+// enough keys (777 tokens 25.3 -> 20.8 us, 2000 of 16 heads of 256 94 -> 71, of 28 heads of
+// 80 54 -> 43; 2048 tokens of 32 heads, 1024 blocks, 53 -> 57, 16 tokens 6.1 -> 6.7);
+// float32 of more than 64 dimensions has no LDS for it (64 -> 74).
+constexpr int kGroupBlocks = 896, kGroupKeys = 512;
 
 PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
   PrPlan pl{};
@@ -433,6 +488,8 @@ PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t
     return std::min<int64_t>(std::max<int64_t>(1, keys / kMinKeys), kMostSplits);
   };
   const int64_t used = ceil_div(N * nq, bm) * Hkv;
+  pl.groups = !wide && used <= kGroupBlocks && keys >= kGroupKeys &&
+                      (dtype == MOE_BF16 || pl.dp == 64) ? 2 : 1;
   const int64_t want = wide ? kWideSplitBlocks : dtype == MOE_F32 ? kFloatSplitBlocks : kSplitBlocks;
   pl.splits = (int)std::min(most(keys), std::max<int64_t>(1, want / used));
   pl.blocks = pl.slots * Hkv * pl.splits;
@@ -458,15 +515,12 @@ bool pr_supported(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int3
 
 template <typename Tv, int DP>
 int pr_launch(const PrArgs& a, const PrPlan& pl, hipStream_t st) {
-  const dim3 grid((unsigned)pl.blocks), block((unsigned)(64 * pl.waves));
-  if constexpr (sizeof(Tv) == 2) {
-    if (pl.waves == 8) {
-      pr_kernel<Tv, DP, DP == 256 ? 1 : 2, 8><<<grid, block, 0, st>>>(a);
-      MOE_CHECK_LAUNCH();
-      return MOE_OK;
-    }
-  }
-  pr_kernel<Tv, DP, 1, 4><<<grid, block, 0, st>>>(a);
+  const dim3 grid((unsigned)pl.blocks), block((unsigned)(64 * pl.waves * pl.groups));
+  if constexpr (sizeof(Tv) == 2)
+    if (pl.waves == 8) pr_kernel<Tv, DP, DP == 256 ? 1 : 2, 8, 1><<<grid, block, 0, st>>>(a);
+  if (pl.waves == 4 && pl.groups == 1) pr_kernel<Tv, DP, 1, 4, 1><<<grid, block, 0, st>>>(a);
+  if constexpr (sizeof(Tv) == 2 || DP == 64)
+    if (pl.groups == 2) pr_kernel<Tv, DP, 1, 4, 2><<<grid, block, 0, st>>>(a);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }

@@ -182,3 +182,24 @@ def test_offsets_past_32_bits():
     got = ops.prompt_attention(q, k, v)
     ref = ops.prompt_attention(*(to_dev(c[x]) for x in ("q", "k", "v")))
     assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,n,m", [
+    ("bf16", 8, 2, 128, 300, 5000),      # blocks of eight waves, keys split
+    ("bf16", 4, 1, 64, 200, 4200), ("bf16", 8, 2, 256, 70, 4500), ("bf16", 6, 2, 80, 130, 4300),
+    ("bf16", 8, 2, 128, 90, 700),        # two groups of waves
+    ("bf16", 3, 3, 256, 60, 600), ("bf16", 7, 1, 40, 33, 520), ("f32", 4, 2, 64, 50, 600),
+    ("f32", 4, 2, 128, 50, 600)])
+def test_every_kind_of_block(dtype, Hq, Hkv, D, n, m):
+    c, g = _case(dtype, [n, 3, 0, 40], [m, m + 9, 5, m - 100], Hq, Hkv, D, n + m + D)
+    rows = set(range(0, 12)) | set(range(n - 9, n + 14)) | {n // 2, n + 42}
+    _check(c, dtype, D ** -0.5, rows=rows)
+    # a value that is no number is seen from its token on
+    v = to_dev(c["v"])
+    at = m - n // 2
+    v[at, 0, D - 3] = float("nan")
+    out, _ = ops.prompt_attention(to_dev(c["q"]), to_dev(c["k"]), v, q_offsets=to_dev(c["qo"]),
+                                  k_offsets=to_dev(c["ko"]))
+    first = at - (m - n)
+    bad = torch.isnan(out)
+    assert bad[first:n, :Hq // Hkv, D - 3].all() and bad.sum() == (n - first) * (Hq // Hkv)
