@@ -49,9 +49,11 @@ extern "C" {
  * workspace  moe_prompt_attention_workspace bytes, 256-byte aligned (may be 0); a size
  *      that does not fall as N, M or B grows: that of the largest call serves all
  * Limits: N >= 1, M >= 0, B >= 1, Hq a multiple of Hkv, D a multiple of 8 up to
- *   256; N * Hq, M, B < 2^31; strides a multiple of 16 bytes, at most 2^24
- *   elements; tensors of dtype on 16 bytes; N * Hq / 32 + B * Hkv below 2^22;
- *   |scale| up to 2.3e38 (below 1e-37 it counts as 0).
+ *   256, Hq <= 65536; N * Hq, B < 2^31, M <= 2^30; strides a multiple of 16 bytes, at
+ *   most 2^24 elements; tensors of dtype on 16 bytes; N * Hq / 32 + B * Hkv below
+ *   2^22; |scale| up to 2.3e38 (below 1e-37 it counts as 0). Outputs and workspace
+ *   whose ranges meet those of inputs or each other are MOE_ERR_ARG, in this and the
+ *   other calls.
  * Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_prompt_attention_workspace(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv,
@@ -73,7 +75,8 @@ int moe_prompt_attention(const void* q, const void* k, const void* v, int32_t dt
  * codes  [n_slots, Hkv, D / 2] uint8: channel 2i in the lower half of byte i, 2i + 1 in
  *        the upper; bit 3 the sign, bits 0..2 the index of the value
  * scales [n_slots, Hkv, D / 32] uint8: e + 127, or 255 for a block of NaN
- * moe_kv_gather and moe_beam_reorder move such caches like any other.
+ * moe_kv_gather and moe_beam_reorder move such caches like any other (codes and scales
+ * in calls of their own, as their bytes a position differ).
  *
  * moe_kv4_store -- tokens 0 .. N-1 of k and v into slots slots[n].
  * moe_kv4_load  -- slots slots[n] back into tokens 0 .. N-1 of k and v, dtype. Every

@@ -38,7 +38,7 @@ def prompt_attention(q, k, v, q_offsets, k_offsets, scale, out=None, lse=None):
 def kv4_encode(x):
     """x [..., D] float -> (codes [..., D/2], scales [..., D/32]) uint8."""
     x = np.asarray(x, dtype=np.float64)
-    y = x.reshape(x.shape[:-1] + (-1, 32))
+    y = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
     codes = np.zeros(y.shape, dtype=np.uint8)
     scales = np.zeros(y.shape[:-1], dtype=np.uint8)
     for at in np.ndindex(scales.shape):

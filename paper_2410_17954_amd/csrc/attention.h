@@ -166,7 +166,8 @@ attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
     __syncthreads();
   }
   if (g != 0 || !mine) return;
-  o *= l == 0.f ? 0.f : 1.f / l;
+  if (l == 0.f) o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  else o *= 1.f / l;
   put4(static_cast<Tv*>(a.out) + at * a.D + d, o);
   if (a.lse && d == 0) a.lse[at] = lse_of(m, l);
 }

@@ -284,7 +284,7 @@ ka_kernel(KaArgs a) {
   char* const units = mine + 2 * C::kSlot;
   uint32_t off[2][C::NI];
   C::offsets(off, a);
-  const int steps = (hi - lo + KEYS - 1) / KEYS;
+  const int steps = (int)(((uint32_t)(hi - lo) + KEYS - 1) / KEYS);
   auto load = [&](int x, int st) {               // keys (x = 0) or values (1) of a step
     const int key = lo + st * KEYS;
     C::load(mine_at + x * C::kSlot, a.codes[x] + base * 16, a.scales[x] + base, key,
@@ -381,13 +381,14 @@ ka_kernel(KaArgs a) {
     if (a.splits > 1) a.part_ml[to] = make_float2(top, l);
     else if (a.lse) a.lse[at] = lse_of(top, l);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = 1.f / l;                     // of no weight: 0, whatever the values hold
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
     const int d = 16 * dt + 4 * q4;              // D is a multiple of 32
     if (d >= a.D) continue;
     if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part_o + to * a.D + d) = o[0][dt];
-    else put4(static_cast<Tv*>(a.out) + at * a.D + d, o[0][dt] * inv);
+    else put4(static_cast<Tv*>(a.out) + at * a.D + d,
+              l == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : o[0][dt] * inv);
   }
 }
 

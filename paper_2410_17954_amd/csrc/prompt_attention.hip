@@ -436,11 +436,14 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
     for (int dt = 0; dt < DT; ++dt) {
       const int d = 16 * dt + 4 * q4;            // D is a multiple of 8
       if (d >= a.D) continue;
-      f32x4_t x = o[i][dt] * f;
+      f32x4_t x = {0.f, 0.f, 0.f, 0.f};          // of no weight, whatever the values hold
+      if (l != 0.f) {
+        x = o[i][dt] * f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (last[i] >= s_up[d + e]) x[e] += INFINITY;
-        if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
+        for (int e = 0; e < 4; ++e) {
+          if (last[i] >= s_up[d + e]) x[e] += INFINITY;
+          if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
+        }
       }
       if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part_o + to * a.D + d) = x;
       else put4(static_cast<Tv*>(a.out) + to * a.D + d, x);
@@ -492,6 +495,9 @@ PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t
                       (dtype == MOE_BF16 || pl.dp == 64) ? 2 : 1;
   const int64_t want = wide ? kWideSplitBlocks : dtype == MOE_F32 ? kFloatSplitBlocks : kSplitBlocks;
   pl.splits = (int)std::min(most(keys), std::max<int64_t>(1, want / used));
+  // a launch's threads are below 2^32; the slots are more than the tiles where sequences
+  // are empty
+  if (pl.slots * Hkv * pl.splits >= ((int64_t)1 << 32) / 512) pl.splits = 1;
   pl.blocks = pl.slots * Hkv * pl.splits;
   // Splits of all rows are at most as many rows as the blocks have columns: `total` allows
   // every call for that many, and never falls as a call grows.
@@ -509,7 +515,7 @@ bool pr_ok(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, 
 }
 bool pr_supported(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D) {
   const int64_t lim = (int64_t)1 << 31;
-  return D % 8 == 0 && D <= 256 && N < lim / Hq && M < lim && B < lim &&
+  return D % 8 == 0 && D <= 256 && N < lim / Hq && M <= lim / 2 && B < lim &&
          (int64_t)Hq * D <= (1 << 24) && Hq <= (1 << 16) && N * Hq / 32 + (double)B * Hkv < (1 << 22);
 }
 

@@ -231,3 +231,18 @@ def test_attention_cache_past_32_bits():
     bound = (p[..., None] * vv.double().cpu().abs().permute(1, 0, 2)).sum(1) / total[:, None] * 2 ** -6
     assert ((out[0].double().cpu() - ref).abs() <= bound).all()
     assert (lse[0].double().cpu() - total.log()).abs().max() <= 2 ** -6
+
+
+@pytest.mark.parametrize("S", [50, 700])
+def test_attention_of_scores_that_are_all_minus_infinity(S):
+    # an infinite query against keys of one sign: no weight, whatever the values hold
+    cache = ops.kv4_cache(1, S, 1, 64, "cuda:0")
+    k = torch.zeros((S, 1, 64), device="cuda:0")
+    k[:, :, 0] = 1.0
+    ops.kv4_store(k, torch.randn_like(k), cache)
+    cache[3][:, ::5] = 255
+    q = torch.zeros((1, 2, 64), device="cuda:0")
+    q[:, 0, 0] = -3e38                               # times 1e3: -inf
+    out, lse = ops.kv4_attention(q.bfloat16(), cache, scale=1e3)
+    assert (out[0, 0] == 0).all() and lse[0, 0] == -float("inf")
+    assert torch.isnan(out[0, 1]).all() and abs(float(lse[0, 1]) - np.log(S)) < 1e-5

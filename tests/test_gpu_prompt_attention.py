@@ -203,3 +203,30 @@ def test_every_kind_of_block(dtype, Hq, Hkv, D, n, m):
     first = at - (m - n)
     bad = torch.isnan(out)
     assert bad[first:n, :Hq // Hkv, D - 3].all() and bad.sum() == (n - first) * (Hq // Hkv)
+
+
+def test_more_sequences_than_tiles():
+    # most of them empty; the others' keys would be split over blocks
+    c, g = _case("bf16", [1, 2], [3000, 2000], 4, 1, 64, 77)
+    B = 70000
+    qo, ko = np.zeros(B + 1, np.int32), np.zeros(B + 1, np.int32)
+    qo[30000:], ko[30000:] = 1, 3000
+    qo[69000:], ko[69000:] = 3, 5000
+    got = ops.prompt_attention(*(to_dev(c[n]) for n in ("q", "k", "v")), q_offsets=to_dev(qo),
+                               k_offsets=to_dev(ko))
+    ref = ops.prompt_attention(*(to_dev(c[n]) for n in ("q", "k", "v")), q_offsets=to_dev(c["qo"]),
+                               k_offsets=to_dev(c["ko"]))
+    # in other splits: roundings of numerators and results of at most 1
+    assert (got[0].float() - ref[0].float()).abs().max() <= 2.0 ** -7
+    assert (got[1] - ref[1]).abs().max() <= 2.0 ** -14
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,m", [(70, 70), (40, 900), (3, 3000)])
+def test_no_weight_whatever_the_values_hold(n, m, dtype):
+    c, _ = _case(dtype, [n], [m], 4, 2, 64, n)
+    q, k, v = (to_dev(c[x]) for x in ("q", "k", "v"))
+    q[:, :, 0], k[:, :, 0] = 1.0, float("-inf")
+    v[::3, 0, 5], v[::7, 1, 6], v[m - 1, 0, 7] = float("nan"), float("inf"), float("nan")
+    out, lse = ops.prompt_attention(q, k, v)
+    assert (out == 0).all() and (lse == -float("inf")).all()

@@ -251,3 +251,15 @@ def test_oracle_logprobs_closed_forms():
     lp, en, top, tl = oracle.token_logprobs(z, np.zeros((3, 1), int), 2)
     assert lp[0, 0] == -np.inf and en[0] == 0 and np.isnan(lp[1:]).all() and np.isnan(en[1:]).all()
     assert (top == -1).all() and (tl == -np.inf).all()
+
+
+def test_prompt_kernels_spill_nothing():
+    # launches of a few microseconds, or loops whose reloads would wait on their loads
+    from test_kernel_resources import _kernels
+    kernels = _kernels()
+    for name in ("pr_kernel", "ka_kernel", "kv4_store_kernel", "kv4_load_kernel", "lp_kernel",
+                 "attention_join_kernel"):
+        mine = {n: (k[".vgpr_spill_count"], k[".private_segment_fixed_size"])
+                for n, k in kernels.items() if name in n}
+        assert mine, name
+        assert not {n: v for n, v in mine.items() if any(v)}
