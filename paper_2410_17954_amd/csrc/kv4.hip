@@ -1,8 +1,9 @@
 // A cache of keys and values in 4 bits: moe_kv4_store, moe_kv4_load.
 //
-// Both are copies bound by HBM. A thread takes 8 channels (16 bytes of bf16 <-> one
-// word of codes), four neighbouring threads a block of 32; they find its largest
-// magnitude with two moves within a quad, and the first of them writes the scale.
+// Both are copies bound by HBM. A thread takes 8 channels of a key and of its value (16
+// bytes of bf16 <-> one word of codes), four neighbouring threads a block of 32; they
+// find its largest magnitude with two moves within a quad, and the first of them writes
+// the scale.
 #include "moeflow_prompt.h"
 #include "common.h"
 #include "rows.h"
@@ -21,7 +22,7 @@ struct Kv4Args {
   const void *k, *v;                             // of a load: written
   uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
   const int32_t* slots;
-  int64_t N, n_slots, k_stride, v_stride, pieces; // pieces: of 8 channels, of k or of v
+  int64_t N, n_slots, k_stride, v_stride, pieces; // pieces: of 8 channels, of k, and of v
   int row;                                       // pieces of a token
 };
 
@@ -93,44 +94,54 @@ template <> struct Eight<float> {
   }
 };
 
+// Piece, token and slot of a thread; false: nothing to do. A block's four threads share a
+// token.
+__device__ __forceinline__ bool kv4_find(const Kv4Args& a, int64_t& n, uint32_t& c, int64_t& slot) {
+  const uint32_t at = blockIdx.x * (uint32_t)kThreads + threadIdx.x;
+  if (at >= (uint32_t)a.pieces) return false;
+  n = at / (uint32_t)a.row;
+  c = at - (uint32_t)n * (uint32_t)a.row;
+  slot = a.slots ? a.slots[n] : n;
+  return slot >= 0 && slot < a.n_slots;
+}
+
 template <typename Tv>
 __global__ void __launch_bounds__(kThreads) kv4_store_kernel(Kv4Args a) {
-  const int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x;
-  if (at >= 2 * a.pieces) return;
-  const bool second = at >= a.pieces;
-  const int64_t i = second ? at - a.pieces : at, n = i / a.row, c = i % a.row;
-  const int64_t slot = a.slots ? a.slots[n] : n;
-  if (slot < 0 || slot >= a.n_slots) return;     // a block's four threads share a token
-  float x[8];
-  Eight<Tv>::get(static_cast<const Tv*>(second ? a.v : a.k) +
-                     n * (second ? a.v_stride : a.k_stride) + c * 8, x);
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-  top = max(top, (uint32_t)dpp<0xB1>((int)top));
-  top = max(top, (uint32_t)dpp<0x4E>((int)top));
-  const int s = kv4_scale(top);
-  const uint32_t w = s == kNaNScale ? 0 : kv4_codes(x, __uint_as_float((uint32_t)s << 23));
+  int64_t n, slot;
+  uint32_t c;
+  if (!kv4_find(a, n, c, slot)) return;
+  float x[2][8];
+  Eight<Tv>::get(static_cast<const Tv*>(a.k) + n * a.k_stride + c * 8, x[0]);
+  Eight<Tv>::get(static_cast<const Tv*>(a.v) + n * a.v_stride + c * 8, x[1]);
   const int64_t to = slot * a.row + c;
-  reinterpret_cast<uint32_t*>(second ? a.v_codes : a.k_codes)[to] = w;
-  if ((c & 3) == 0) (second ? a.v_scales : a.k_scales)[to >> 2] = (uint8_t)s;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[i][j]) & 0x7fffffffu);
+    top = max(top, (uint32_t)dpp<0xB1>((int)top));
+    top = max(top, (uint32_t)dpp<0x4E>((int)top));
+    const int s = kv4_scale(top);
+    reinterpret_cast<uint32_t*>(i ? a.v_codes : a.k_codes)[to] =
+        s == kNaNScale ? 0 : kv4_codes(x[i], __uint_as_float((uint32_t)s << 23));
+    if ((c & 3) == 0) (i ? a.v_scales : a.k_scales)[to >> 2] = (uint8_t)s;
+  }
 }
 
 template <typename Tv>
 __global__ void __launch_bounds__(kThreads) kv4_load_kernel(Kv4Args a) {
-  const int64_t at = blockIdx.x * (int64_t)kThreads + threadIdx.x;
-  if (at >= 2 * a.pieces) return;
-  const bool second = at >= a.pieces;
-  const int64_t i = second ? at - a.pieces : at, n = i / a.row, c = i % a.row;
-  const int64_t slot = a.slots ? a.slots[n] : n;
-  if (slot < 0 || slot >= a.n_slots) return;
+  int64_t n, slot;
+  uint32_t c;
+  if (!kv4_find(a, n, c, slot)) return;
   const int64_t from = slot * a.row + c;
-  const uint32_t w = reinterpret_cast<const uint32_t*>(second ? a.v_codes : a.k_codes)[from];
-  const uint32_t s = (second ? a.v_scales : a.k_scales)[from >> 2];
+  const uint32_t wk = reinterpret_cast<const uint32_t*>(a.k_codes)[from];
+  const uint32_t wv = reinterpret_cast<const uint32_t*>(a.v_codes)[from];
+  const uint32_t sk = a.k_scales[from >> 2], sv = a.v_scales[from >> 2];
   float x[8];
-  kv4_values(w, s, x);
-  Eight<Tv>::put(const_cast<Tv*>(static_cast<const Tv*>(second ? a.v : a.k)) +
-                     n * (second ? a.v_stride : a.k_stride) + c * 8, x);
+  kv4_values(wk, sk, x);
+  Eight<Tv>::put(const_cast<Tv*>(static_cast<const Tv*>(a.k)) + n * a.k_stride + c * 8, x);
+  kv4_values(wv, sv, x);
+  Eight<Tv>::put(const_cast<Tv*>(static_cast<const Tv*>(a.v)) + n * a.v_stride + c * 8, x);
 }
 
 int kv4_run(bool load, int32_t dtype, const Kv4Args& a, int32_t Hkv, int32_t D, void* stream) {
@@ -166,7 +177,7 @@ int kv4_run(bool load, int32_t dtype, const Kv4Args& a, int32_t Hkv, int32_t D, 
   Kv4Args b = a;
   b.row = (int)(row / 8);
   b.pieces = a.N * b.row;
-  const dim3 grid((unsigned)ceil_div(2 * b.pieces, kThreads));
+  const dim3 grid((unsigned)ceil_div(b.pieces, kThreads));
   hipStream_t st = as_stream(stream);
   if (load) {
     if (dtype == MOE_BF16) kv4_load_kernel<uint16_t><<<grid, dim3(kThreads), 0, st>>>(b);

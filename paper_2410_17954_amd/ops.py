@@ -1068,14 +1068,15 @@ def kv4_cache(rows, positions, Hkv, D, device):
 
 
 def _kv4_shape(cache):
-    torch = _torch()
     kc, ks, vc, vs = cache
     if kc.dim() != 4:
         raise ValueError("a cache's codes must be [rows, positions, Hkv, D // 2]")
     C, S, Hkv, half = kc.shape
-    for name, t, w in (("k_codes", kc, half), ("v_codes", vc, half), ("k_scales", ks, half // 16),
-                       ("v_scales", vs, half // 16)):
-        _want(name, t, (C, S, Hkv, w), torch.uint8)
+    u8, scales = _torch().uint8, (C, S, Hkv, half // 16)
+    if vc.shape != kc.shape or ks.shape != scales or vs.shape != scales or kc.dtype != u8 \
+            or vc.dtype != u8 or ks.dtype != u8 or vs.dtype != u8:
+        raise ValueError("a cache is uint8: codes [rows, positions, Hkv, D // 2], scales "
+                         "[rows, positions, Hkv, D // 32], of keys and of values")
     return C, S, Hkv, 2 * half
 
 
