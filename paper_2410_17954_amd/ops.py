@@ -745,23 +745,24 @@ def _one_device(stream, *ts, strided=()):
     dev = -1
     for t in strided:
         d = t.get_device()
-        if d < 0:
-            raise ValueError("every tensor must be on the GPU")
-        if dev >= 0 and d != dev:
-            raise ValueError("every tensor must be on the same GPU")
-        dev = d
+        if d != dev:
+            if d < 0:
+                raise ValueError("every tensor must be on the GPU")
+            if dev >= 0:
+                raise ValueError("every tensor must be on the same GPU")
+            dev = d
     for t in ts:
         if t is None:
             continue
         d = t.get_device()
-        if d < 0:
-            raise ValueError("every tensor must be on the GPU")
+        if d != dev:
+            if d < 0:
+                raise ValueError("every tensor must be on the GPU")
+            if dev >= 0:
+                raise ValueError("every tensor must be on the same GPU")
+            dev = d
         if not t.is_contiguous():
             raise ValueError("every tensor must be contiguous")
-        if dev < 0:
-            dev = d
-        elif d != dev:
-            raise ValueError("every tensor must be on the same GPU")
     cuda = _torch().cuda
     if stream is not None:
         if stream.device.index != dev:
@@ -998,13 +999,17 @@ def beam_reorder(caches, parent, lens=None, new_lens=None, err=None, stream=None
 # --------------------------------------------- prompts, a cache in 4 bits, logprobs
 def _token_stride(name, t, heads, width):
     """Elements between the tokens of t [n, heads, width], whose tokens are packed."""
-    if t.shape[1:] != (heads, width):
+    n, h, w = t.shape
+    if h != heads or w != width:
         raise ValueError(f"{name} must be [tokens, {heads}, {width}]")
-    if t.numel() == 0 or t.is_contiguous():
+    if n <= 1 or t.is_contiguous():
+        if n == 1 and not t.is_contiguous():
+            raise ValueError(f"{name}: the heads and channels of a token must be packed")
         return heads * width
-    if (width > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != width):
+    st = t.stride()
+    if (width > 1 and st[2] != 1) or (heads > 1 and st[1] != width):
         raise ValueError(f"{name}: the heads and channels of a token must be packed")
-    return heads * width if t.shape[0] == 1 else t.stride(0)
+    return st[0]
 
 
 def prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code=MOE_BF16):
