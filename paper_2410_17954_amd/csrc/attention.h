@@ -106,17 +106,19 @@ struct JoinArgs {
   float* lse;
 };
 
+constexpr int kJoinBlocks = 512;
+
 namespace {                                      // a kernel of its own for every source
 
-// Block of T threads: tpr of them (at least D / 4) take four dimensions each of a row
-// and head, the T / rows_per_block / tpr groups of them share the splits; all powers of
-// two. Groups are added up in a tree: a fixed order. These launches are latency, so a
-// thread's loads do not wait for each other: the maximum over all splits comes first.
+// Block of T threads: tpr of them (at least D / 4; 16, 32 or 64) take four dimensions each
+// of a row and head, sg groups of them share the splits (a power of two; groups are
+// added up in a tree: a fixed order). A thread's loads do not wait for each other: the
+// maximum over all splits comes first.
 template <typename Tv, int T>
 __global__ void __launch_bounds__(T)
 attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
   __shared__ f32x4_t s_o[T];
-  __shared__ float s_l[T], s_m[T];
+  __shared__ float s_l[T];
   const int tpr = 1 << tpr_shift, sg = 1 << sg_shift;
   const int64_t at = (int64_t)blockIdx.x * (T >> (tpr_shift + sg_shift)) +
                      (threadIdx.x >> (tpr_shift + sg_shift));
@@ -125,18 +127,21 @@ attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
   bool live = at < a.RH;
   if (a.offsets) live = live && row >= a.offsets[0] && row < a.offsets[a.n_off - 1];
   const bool mine = live && d < a.D;
-  // maximum over the splits: the threads of a row and head share them all
   float m = -INFINITY;
+  auto lanes_max = [&]() {
+    for (int n = tpr >> 1; n > 0; n >>= 1) m = fmaxf(m, __shfl_xor(m, n, kWave));
+  };
   if (live)
     for (int p = g * tpr + x; p < a.splits; p += sg * tpr) m = fmaxf(m, a.part_ml[p * a.RH + at].x);
-  const int first = threadIdx.x & ~((tpr << sg_shift) - 1);
-  s_m[threadIdx.x] = m;
-  __syncthreads();
-  for (int n = tpr << sg_shift >> 1; n > 0; n >>= 1) {
-    if ((int)threadIdx.x - first < n) s_m[threadIdx.x] = fmaxf(s_m[threadIdx.x], s_m[threadIdx.x + n]);
+  lanes_max();
+  if (sg > 1) {
+    const int first = (threadIdx.x >> (tpr_shift + sg_shift)) << sg_shift;
+    if (x == 0) s_l[first + g] = m;
     __syncthreads();
+    for (int i = x; i < sg; i += tpr) m = fmaxf(m, s_l[first + i]);
+    lanes_max();
+    __syncthreads();                             // s_l is rewritten below
   }
-  m = s_m[first];
   const float mu = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   f32x4_t o = {0.f, 0.f, 0.f, 0.f};
@@ -177,9 +182,11 @@ int attention_join_with(const JoinArgs& a, hipStream_t st) {
   const int tpr_shift = a.D <= 64 ? 4 : a.D <= 128 ? 5 : 6;
   int t_shift = 0, sg_shift = 0;
   while ((1 << t_shift) < T) ++t_shift;
-  while (sg_shift < t_shift - tpr_shift && (2 << sg_shift) <= a.splits) ++sg_shift;
-  const int64_t blocks = ceil_div(a.RH, T >> (tpr_shift + sg_shift));
-  attention_join_kernel<Tv, T><<<dim3((unsigned)blocks), dim3(T), 0, st>>>(a, tpr_shift, sg_shift);
+  // groups until the card has blocks enough: with many rows threads take all splits
+  auto blocks = [&]() { return ceil_div(a.RH, T >> (tpr_shift + sg_shift)); };
+  while (sg_shift < t_shift - tpr_shift && (2 << sg_shift) <= a.splits && blocks() < kJoinBlocks)
+    ++sg_shift;
+  attention_join_kernel<Tv, T><<<dim3((unsigned)blocks()), dim3(T), 0, st>>>(a, tpr_shift, sg_shift);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }
