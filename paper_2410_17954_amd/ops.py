@@ -738,19 +738,11 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
 _CURRENT = contextlib.nullcontext()
 
 
-def _one_device(stream, *ts, strided=()):
-    """Every given tensor on one GPU, those of ts contiguous: a context in which that
-    is the current device and `stream`, if there is one, the current stream, so that
-    what the call allocates or fills belongs to the stream that it goes to."""
+def _one_device(stream, *ts):
+    """Every given tensor contiguous, on one GPU: a context in which that is the
+    current device and `stream`, if there is one, the current stream, so that what
+    the call allocates or fills belongs to the stream that it goes to."""
     dev = -1
-    for t in strided:
-        d = t.get_device()
-        if d != dev:
-            if d < 0:
-                raise ValueError("every tensor must be on the GPU")
-            if dev >= 0:
-                raise ValueError("every tensor must be on the same GPU")
-            dev = d
     for t in ts:
         if t is None:
             continue
@@ -1012,6 +1004,41 @@ def _token_stride(name, t, heads, width):
     return st[0]
 
 
+def _checked(stream, strided, *specs):
+    """_one_device and _want in one pass, for calls whose time is the host's. specs:
+    (name, tensor or None, shape or None, dtype or None), contiguous; strided: tensors
+    whose layout has been checked."""
+    dev = -1
+    for t in strided:
+        d = t.get_device()
+        if d != dev:
+            if d < 0:
+                raise ValueError("every tensor must be on the GPU")
+            if dev >= 0:
+                raise ValueError("every tensor must be on the same GPU")
+            dev = d
+    for name, t, shape, dtype in specs:
+        if t is None:
+            continue
+        if (dtype is not None and t.dtype != dtype) or (shape is not None and t.shape != shape):
+            raise ValueError(f"{name} must be {dtype} {'' if shape is None else list(shape)}")
+        d = t.get_device()
+        if d != dev:
+            if d < 0:
+                raise ValueError("every tensor must be on the GPU")
+            if dev >= 0:
+                raise ValueError("every tensor must be on the same GPU")
+            dev = d
+        if not t.is_contiguous():
+            raise ValueError("every tensor must be contiguous")
+    cuda = _torch().cuda
+    if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError("the stream must be of the tensors' GPU")
+        return cuda.stream(stream)
+    return _CURRENT if dev == cuda.current_device() else cuda.device(dev)
+
+
 def prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code=MOE_BF16):
     return load_library().moe_prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code)
 
@@ -1028,9 +1055,9 @@ def prompt_attention(q, k, v, q_offsets=None, k_offsets=None, scale=None, out=No
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise ValueError("q must be [N, Hq, D], k and v [M, Hkv, D]")
     N, Hq, D = q.shape
-    M, Hkv = k.shape[:2]
-    dt = _dtype_code(q)
-    if k.dtype != q.dtype or v.dtype != q.dtype or v.shape[0] != M:
+    M, Hkv, _ = k.shape
+    dt, dtype, i32 = _dtype_code(q), q.dtype, torch.int32
+    if k.dtype != dtype or v.dtype != dtype or v.shape[0] != M:
         raise ValueError("q, k and v must have one dtype, k and v one length")
     qs = _token_stride("q", q, Hq, D)
     ks, vs = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
@@ -1039,25 +1066,24 @@ def prompt_attention(q, k, v, q_offsets=None, k_offsets=None, scale=None, out=No
         if q_offsets.dim() != 1 or q_offsets.shape[0] < 2:
             raise ValueError("q_offsets must be [B+1]")
         B = q_offsets.shape[0] - 1
-        _want("q_offsets", q_offsets, (B + 1,), torch.int32)
         if k_offsets is None and B > 1 and M != N:
             raise ValueError("k_offsets are needed where keys and queries differ")
-    _want("k_offsets", k_offsets, (B + 1,), torch.int32)
-    _want("out", out, (N, Hq, D), q.dtype)
-    _want("lse", lse, (N, Hq), torch.float32)
-    with _one_device(stream, q_offsets, k_offsets, out, lse, workspace, strided=(q, k, v)):
+    with _checked(stream, (q, k, v), ("q_offsets", q_offsets, None, i32),
+                  ("k_offsets", k_offsets, (B + 1,), i32), ("out", out, (N, Hq, D), dtype),
+                  ("lse", lse, (N, Hq), torch.float32), ("workspace", workspace, None, None)):
         if out is None:                # rows of no sequence are left as they are
             new = torch.empty if q_offsets is None else torch.zeros
-            out = new((N, Hq, D), dtype=q.dtype, device=q.device)
+            out = new((N, Hq, D), dtype=dtype, device=q.device)
         if lse is None and want_lse:
             lse = torch.full((N, Hq), -float("inf"), dtype=torch.float32, device=q.device)
         ws, nbytes = _scratch(workspace, q.device, lib.moe_prompt_attention_workspace, N, M, B, Hq,
                               Hkv, D, dt)
         st = lib.moe_prompt_attention(
-            _addr(q), _addr(k), _addr(v), dt, N, M, B, Hq, Hkv, D, qs, ks, vs, _addr(q_offsets),
-            _addr(k_offsets), float(D ** -0.5 if scale is None else scale), _addr(out), _addr(lse),
-            _addr(ws), nbytes, _raw_stream())
-    _check("moe_prompt_attention", st)
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), dt, N, M, B, Hq, Hkv, D, qs, ks, vs,
+            _addr(q_offsets), _addr(k_offsets), float(D ** -0.5 if scale is None else scale),
+            out.data_ptr(), _addr(lse), _addr(ws), nbytes, _raw_stream())
+    if st:
+        _check("moe_prompt_attention", st)
     return out, lse
 
 
@@ -1093,16 +1119,19 @@ def kv4_store(k, v, cache, slots=None, stream=None):
     lib = load_library()
     if k.dim() != 3 or v.dim() != 3 or k.dtype != v.dtype or k.shape[0] != v.shape[0]:
         raise ValueError("k and v must be [N, Hkv, D] of one dtype")
-    N = k.shape[0]
     C, S, Hkv, D = _kv4_shape(cache)
     dt = _dtype_code(k)
     kst, vst = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
-    _want("slots", slots, (N,), torch.int32)
+    N, u8 = k.shape[0], torch.uint8
     kc, ks, vc, vs = cache
-    with _one_device(stream, *cache, slots, strided=(k, v)):
-        st = lib.moe_kv4_store(_addr(k), _addr(v), dt, N, Hkv, D, kst, vst, _addr(slots), C * S,
-                               _addr(kc), _addr(ks), _addr(vc), _addr(vs), _raw_stream())
-    _check("moe_kv4_store", st)
+    with _checked(stream, (k, v), ("k_codes", kc, None, u8), ("k_scales", ks, None, u8),
+                  ("v_codes", vc, None, u8), ("v_scales", vs, None, u8),
+                  ("slots", slots, (N,), torch.int32)):
+        st = lib.moe_kv4_store(k.data_ptr(), v.data_ptr(), dt, N, Hkv, D, kst, vst, _addr(slots),
+                               C * S, kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(),
+                               _raw_stream())
+    if st:
+        _check("moe_kv4_store", st)
 
 
 def kv4_load(cache, slots=None, k=None, v=None, dtype=None, stream=None):
@@ -1116,23 +1145,27 @@ def kv4_load(cache, slots=None, k=None, v=None, dtype=None, stream=None):
     if (k is None) != (v is None):
         raise ValueError("keys and values go together")
     N = slots.shape[0] if slots is not None else k.shape[0] if k is not None else C * S
-    _want("slots", slots, (N,), torch.int32)
     if k is not None:
         if k.dim() != 3 or v.dim() != 3 or k.dtype != v.dtype or k.shape[0] != N or v.shape[0] != N:
             raise ValueError("k and v must be [N, Hkv, D] of one dtype")
         if dtype is not None and dtype != k.dtype:
             raise ValueError("dtype differs from that of k and v")
     kc, ks, vc, vs = cache
-    with _one_device(stream, *cache, slots, strided=() if k is None else (k, v)):
+    u8 = torch.uint8
+    with _checked(stream, () if k is None else (k, v), ("k_codes", kc, None, u8),
+                  ("k_scales", ks, None, u8), ("v_codes", vc, None, u8), ("v_scales", vs, None, u8),
+                  ("slots", slots, (N,), torch.int32)):
         if k is None:
             new = torch.empty if slots is None else torch.zeros
             k, v = (new((N, Hkv, D), dtype=dtype or torch.bfloat16, device=kc.device)
                     for _ in range(2))
         dt = _dtype_code(k)
         kst, vst = _token_stride("k", k, Hkv, D), _token_stride("v", v, Hkv, D)
-        st = lib.moe_kv4_load(_addr(kc), _addr(ks), _addr(vc), _addr(vs), C * S, _addr(slots), N,
-                              Hkv, D, dt, kst, vst, _addr(k), _addr(v), _raw_stream())
-    _check("moe_kv4_load", st)
+        st = lib.moe_kv4_load(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), C * S,
+                              _addr(slots), N, Hkv, D, dt, kst, vst, k.data_ptr(), v.data_ptr(),
+                              _raw_stream())
+    if st:
+        _check("moe_kv4_load", st)
     return k, v
 
 
@@ -1154,23 +1187,25 @@ def kv4_attention(q, cache, lens=None, cache_row=None, scale=None, out=None, lse
     C, S, Hkv, width = _kv4_shape(cache)
     if width != D:
         raise ValueError("q and the cache differ in D")
-    dt = _dtype_code(q)
-    _want("lens", lens, (R,), torch.int32)
-    _want("cache_row", cache_row, (R,), torch.int32)
-    _want("out", out, (R, Hq, D), q.dtype)
-    _want("lse", lse, (R, Hq), torch.float32)
+    dt, dtype, i32, u8 = _dtype_code(q), q.dtype, torch.int32, torch.uint8
     kc, ks, vc, vs = cache
-    with _one_device(stream, q, *cache, lens, cache_row, out, lse, workspace):
+    with _checked(stream, (), ("q", q, None, dtype), ("k_codes", kc, None, u8),
+                  ("k_scales", ks, None, u8), ("v_codes", vc, None, u8), ("v_scales", vs, None, u8),
+                  ("lens", lens, (R,), i32), ("cache_row", cache_row, (R,), i32),
+                  ("out", out, (R, Hq, D), dtype), ("lse", lse, (R, Hq), torch.float32),
+                  ("workspace", workspace, None, None)):
         if out is None:
             out = torch.empty_like(q)
         if lse is None and want_lse:
             lse = torch.empty((R, Hq), dtype=torch.float32, device=q.device)
         ws, nbytes = _scratch(workspace, q.device, lib.moe_kv4_attention_workspace, R, S, Hq, Hkv, D)
         st = lib.moe_kv4_attention(
-            _addr(q), dt, R, Hq, Hkv, D, _addr(kc), _addr(ks), _addr(vc), _addr(vs), C, S,
-            _addr(cache_row), _addr(lens), float(D ** -0.5 if scale is None else scale), _addr(out),
-            _addr(lse), _addr(ws), nbytes, _raw_stream())
-    _check("moe_kv4_attention", st)
+            q.data_ptr(), dt, R, Hq, Hkv, D, kc.data_ptr(), ks.data_ptr(), vc.data_ptr(),
+            vs.data_ptr(), C, S, _addr(cache_row), _addr(lens),
+            float(D ** -0.5 if scale is None else scale), out.data_ptr(), _addr(lse), _addr(ws),
+            nbytes, _raw_stream())
+    if st:
+        _check("moe_kv4_attention", st)
     return out, lse
 
 
@@ -1194,33 +1229,33 @@ def token_logprobs(logits, tokens=None, n_top=0, logprobs=None, entropy=None, wa
     if V > 1 and logits.stride(1) != 1:
         raise ValueError("the logits of a row must be packed")
     stride = V if R == 1 else logits.stride(0)
-    if tokens is not None and tokens.dim() != 2:
-        raise ValueError("tokens must be [R, m]")
-    m = 0 if tokens is None else tokens.shape[1]
-    _want("tokens", tokens, (R, m), torch.int32)
-    if logprobs is not None and tokens is None:
+    m = 0
+    if tokens is not None:
+        if tokens.dim() != 2:
+            raise ValueError("tokens must be [R, m]")
+        m = tokens.shape[1]
+    elif logprobs is not None:
         raise ValueError("logprobs need tokens")
     if n_top == 0 and (top_tokens is not None or top_logprobs is not None):
         raise ValueError("top_tokens and top_logprobs need n_top")
-    _want("logprobs", logprobs, (R, m), torch.float32)
-    _want("entropy", entropy, (R,), torch.float32)
-    _want("top_tokens", top_tokens, (R, n_top), torch.int32)
-    _want("top_logprobs", top_logprobs, (R, n_top), torch.float32)
-    with _one_device(stream, tokens, logprobs, entropy, top_tokens, top_logprobs, workspace,
-                     strided=(logits,)):
-        new = lambda t, shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device) \
-            if t is None else t
-        if tokens is not None:
-            logprobs = new(logprobs, (R, m), torch.float32)
-        if want_entropy:
-            entropy = new(entropy, (R,), torch.float32)
-        if n_top > 0:
-            top_tokens = new(top_tokens, (R, n_top), torch.int32)
-            top_logprobs = new(top_logprobs, (R, n_top), torch.float32)
-        ws, nbytes = _scratch(workspace, logits.device, lib.moe_token_logprobs_workspace, R, V, m,
-                              n_top)
-        st = lib.moe_token_logprobs(_addr(logits), dt, R, V, stride, _addr(tokens), m, n_top,
+    i32, f32, top = torch.int32, torch.float32, (R, n_top)
+    with _checked(stream, (logits,), ("tokens", tokens, (R, m), i32),
+                  ("logprobs", logprobs, (R, m), f32), ("entropy", entropy, (R,), f32),
+                  ("top_tokens", top_tokens, top, i32), ("top_logprobs", top_logprobs, top, f32),
+                  ("workspace", workspace, None, None)):
+        dev = logits.device
+        if tokens is not None and logprobs is None:
+            logprobs = torch.empty((R, m), dtype=f32, device=dev)
+        if want_entropy and entropy is None:
+            entropy = torch.empty(R, dtype=f32, device=dev)
+        if n_top > 0 and top_tokens is None:
+            top_tokens = torch.empty(top, dtype=i32, device=dev)
+        if n_top > 0 and top_logprobs is None:
+            top_logprobs = torch.empty(top, dtype=f32, device=dev)
+        ws, nbytes = _scratch(workspace, dev, lib.moe_token_logprobs_workspace, R, V, m, n_top)
+        st = lib.moe_token_logprobs(logits.data_ptr(), dt, R, V, stride, _addr(tokens), m, n_top,
                                     _addr(logprobs), _addr(entropy), _addr(top_tokens),
                                     _addr(top_logprobs), _addr(ws), nbytes, _raw_stream())
-    _check("moe_token_logprobs", st)
+    if st:
+        _check("moe_token_logprobs", st)
     return logprobs, entropy, top_tokens, top_logprobs
