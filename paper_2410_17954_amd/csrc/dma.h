@@ -23,7 +23,8 @@ __device__ __forceinline__ u32x4_t dma_rows(const void* base, int64_t first, int
 // SIZE bytes a lane of a raw buffer into LDS: 16 at lds + 16 * lane; 4, 2 or 1 as a word at
 // lds + 4 * lane. Past its end: zeros. The compiler does not see that these are on their
 // way: it would wait for all of them at every transposing read. wait_loads does; loads
-// that the compiler counts as well make its own waits longer, never shorter.
+// that the compiler counts as well make its own waits longer, never shorter. m0 is a register
+// that it reserves and keeps no value in.
 template <int SIZE>
 __device__ __forceinline__ void dma(uint32_t lds, uint32_t voff, u32x4_t rs) {
   if constexpr (SIZE == 16)

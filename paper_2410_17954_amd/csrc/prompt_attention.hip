@@ -119,7 +119,6 @@ __device__ __forceinline__ bool pr_find(const PrArgs& a, PrJob& j) {
   return true;
 }
 
-
 // DP: the dimension padded to rows of whole 128 bytes; 16-byte chunks past D are zeros.
 template <typename Tv, int DP, int kMT, int W, int BN>
 struct PrCore {
@@ -411,12 +410,12 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
     }
     __syncthreads();
     if (group > 0) return;
+#pragma unroll 1
+    for (int g = 1; g < KS; ++g)
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
+      for (int i = 0; i < kMT; ++i)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int g = 1; g < KS; ++g)
+        for (int dt = 0; dt < DT; ++dt)
           o[i][dt] += part[(((any + g * W) * kMT + i) * DT + dt) * kWave + lane];
   } else {
     __syncthreads();
@@ -476,6 +475,14 @@ constexpr int kMinKeys = 128, kMostSplits = 64;
 // 80 54 -> 43; 2048 tokens of 32 heads, 1024 blocks, 53 -> 57, 16 tokens 6.1 -> 6.7);
 // float32 of more than 64 dimensions has no LDS for it (64 -> 74).
 constexpr int kGroupBlocks = 896, kGroupKeys = 512;
+// Four groups where every block has a compute unit to itself, which its LDS takes (32
+// heads of 128: 256 tokens 16.0 -> 11.2 us, 400 20.0 -> 12.8, 512 20.0 -> 13.9; 128 tokens
+// 7.9 -> 9.8; 600, in 304 blocks, 16.0 -> 19.5), and sequences have columns to fill it
+// (16 tokens of two sequences behind 1000 keys 14.5 -> 16.2). A join then costs as much as
+// four tiles a group: splits are of kFourMinKeys at least (512 tokens of 16 heads 12.9 us,
+// in two splits 18.5; of 1024 keys, 40 tokens behind 3000 take 27.2 instead of 20.0).
+// float32, whose splits are more, 31.9 -> 38.5 (1500 tokens of 4 heads of 64).
+constexpr int kFourBlocks = 256, kFourKeys = 256, kFourColumns = 128, kFourMinKeys = 512;
 
 PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
   PrPlan pl{};
@@ -490,14 +497,21 @@ PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t
   auto most = [](int64_t keys) {
     return std::min<int64_t>(std::max<int64_t>(1, keys / kMinKeys), kMostSplits);
   };
-  const int64_t used = ceil_div(N * nq, bm) * Hkv;
+  // blocks of a split, if sequences are alike; those without a token have none
+  const int64_t some = std::min(B, N), cols = ceil_div(N, some) * nq;
+  const int64_t used = some * ceil_div(cols, bm) * Hkv;
   pl.groups = !wide && used <= kGroupBlocks && keys >= kGroupKeys &&
                       (dtype == MOE_BF16 || pl.dp == 64) ? 2 : 1;
-  const int64_t want = wide ? kWideSplitBlocks : dtype == MOE_F32 ? kFloatSplitBlocks : kSplitBlocks;
-  pl.splits = (int)std::min(most(keys), std::max<int64_t>(1, want / used));
+  if (!wide && dtype == MOE_BF16 && pl.dp <= 128 && used <= kFourBlocks && keys >= kFourKeys &&
+      cols >= kFourColumns)
+    pl.groups = 4;
+  const int64_t want = pl.groups == 4 ? kFourBlocks : wide ? kWideSplitBlocks
+                     : dtype == MOE_F32 ? kFloatSplitBlocks : kSplitBlocks;
+  const int64_t fit = pl.groups == 4 ? std::max<int64_t>(1, keys / kFourMinKeys) : most(keys);
+  pl.splits = (int)std::min(std::min(fit, most(keys)), std::max<int64_t>(1, want / used));
   // a launch's threads are below 2^32; the slots are more than the tiles where sequences
   // are empty
-  if (pl.slots * Hkv * pl.splits >= ((int64_t)1 << 32) / 512) pl.splits = 1;
+  if (pl.slots * Hkv * pl.splits >= ((int64_t)1 << 32) / 1024) pl.splits = 1;
   pl.blocks = pl.slots * Hkv * pl.splits;
   // Splits of all rows are at most as many rows as the blocks have columns: `total` allows
   // every call for that many, and never falls as a call grows.
@@ -527,6 +541,8 @@ int pr_launch(const PrArgs& a, const PrPlan& pl, hipStream_t st) {
   if (pl.waves == 4 && pl.groups == 1) pr_kernel<Tv, DP, 1, 4, 1><<<grid, block, 0, st>>>(a);
   if constexpr (sizeof(Tv) == 2 || DP == 64)
     if (pl.groups == 2) pr_kernel<Tv, DP, 1, 4, 2><<<grid, block, 0, st>>>(a);
+  if constexpr (sizeof(Tv) == 2 && DP <= 128)
+    if (pl.groups == 4) pr_kernel<Tv, DP, 1, 4, 4><<<grid, block, 0, st>>>(a);
   MOE_CHECK_LAUNCH();
   return MOE_OK;
 }

@@ -205,6 +205,30 @@ def test_every_kind_of_block(dtype, Hq, Hkv, D, n, m):
     assert bad[first:n, :Hq // Hkv, D - 3].all() and bad.sum() == (n - first) * (Hq // Hkv)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,nq,nk", [
+    ("bf16", 8, 2, 128, [300], [300]),                     # four groups of waves
+    ("bf16", 8, 2, 64, [260, 1, 0], [1500, 400, 7]), ("bf16", 16, 2, 96, [257, 33], [257, 300]),
+    ("bf16", 4, 1, 40, [70], [2100]), ("bf16", 7, 1, 128, [64], [1100]),   # and splits
+    ("bf16", 32, 8, 128, [600], [600]),                    # two
+    ("bf16", 6, 2, 256, [100], [900]), ("bf16", 4, 1, 128, [20], [900]),
+    ("f32", 4, 2, 64, [100, 30], [900, 700])])
+def test_groups_of_waves(dtype, Hq, Hkv, D, nq, nk):
+    c, g = _case(dtype, nq, nk, Hq, Hkv, D, sum(nk) + D)
+    N = sum(nq)
+    rows = set(range(0, 5)) | set(range(nq[0] - 5, nq[0] + 3)) | {nq[0] // 2, N - 1}
+    a = _check(c, dtype, D ** -0.5, rows=rows)
+    b = _check(c, dtype, D ** -0.5, rows={0})
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    v = to_dev(c["v"])
+    at = nk[0] - nq[0] // 2            # a value that is no number is seen from its token on
+    v[at, Hkv - 1, D - 1], first = float("inf"), at - (nk[0] - nq[0])
+    out, _ = ops.prompt_attention(to_dev(c["q"]), to_dev(c["k"]), v, q_offsets=to_dev(c["qo"]),
+                                  k_offsets=to_dev(c["ko"]))
+    bad = out == float("inf")
+    assert bad[first:nq[0], -(Hq // Hkv):, D - 1].all()
+    assert bad.sum() == (nq[0] - first) * (Hq // Hkv) and torch.isfinite(out[~bad]).all()
+
+
 def test_more_sequences_than_tiles():
     # most of them empty; the others' keys would be split over blocks
     c, g = _case("bf16", [1, 2], [3000, 2000], 4, 1, 64, 77)
