@@ -247,8 +247,10 @@ struct PrCore {
   // Values that are no numbers, in a tile that some query does not see as a whole:
   // 0 times them would be NaN. Of the chunks that this wave loaded they become 0, and
   // for every dimension the first key of +inf or NaN and of -inf or NaN is kept: a
-  // query that sees it gets the infinity, or both, at the end.
-  static __device__ __forceinline__ void take_odd(char* tile, int key, int wave, int* up, int* down) {
+  // query that sees it gets the infinity, or both, at the end. *any: there are such
+  // (the end of a block without them is 1 us shorter: 8 tokens 6.2 -> 5.2).
+  static __device__ __forceinline__ void take_odd(char* tile, int key, int wave, int* up, int* down,
+                                                  int* any) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int g = (wave * PIECES + p) * 64 + lane_id(), row = g / CH;
@@ -261,6 +263,7 @@ struct PrCore {
         if constexpr (BF16) odd |= (w[e] & 0x7f80u) == 0x7f80u;
       }
       if (!odd) continue;
+      *any = 1;
       const int d0 = ((g % CH) ^ swz_v(row)) * VE;
       Tv* const x = reinterpret_cast<Tv*>(at);
 #pragma unroll 1
@@ -294,13 +297,14 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
   constexpr int kLds = KS > 1 && KS * kPart > 4 * KS * C::kTile ? KS * kPart : 4 * KS * C::kTile;
   __shared__ __attribute__((aligned(16))) char lds[kLds];
   __shared__ float s_m[KS][W * kMT * 16], s_l[KS][W * kMT * 16];
-  __shared__ int s_up[DP], s_down[DP];
+  __shared__ int s_up[DP], s_down[DP], s_odd;
   PrJob j;
   if (!pr_find<Tv, BM, BN>(a, j)) return;
   const int lane = lane_id(), r = lane & 15, q4 = lane >> 4;
   const int any = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wave = any % W, group = any / W;
   for (int d = threadIdx.x; d < DP; d += 64 * W * KS) s_up[d] = s_down[d] = 0x7fffffff;
+  if (threadIdx.x == 0) s_odd = 0;
   uint32_t off_k[C::PIECES], off_v[C::PIECES];
   C::offsets(off_k, off_v, wave, a);
   char* const ring = lds + group * 4 * C::kTile;
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
   auto tile = [&](auto BUF, int key) {
     char* const tk = ring + BUF * 2 * C::kTile;
     wait_loads<0>();
-    if (key < j.hi && key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down);
+    if (key < j.hi && key + BN > b_all) C::take_odd(tk + C::kTile, key, wave, s_up, s_down, &s_odd);
     // the tile has landed, and every wave is done with the other buffer
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (key + KS * BN < j.hi) load(1 - BUF, key + KS * BN);
@@ -421,6 +425,7 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
     __syncthreads();
   }
   const int64_t RH = a.N * a.Hq;
+  const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
     const float l = l_all[i];
@@ -438,10 +443,12 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
       f32x4_t x = {0.f, 0.f, 0.f, 0.f};          // of no weight, whatever the values hold
       if (l != 0.f) {
         x = o[i][dt] * f;
+        if (odd) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (last[i] >= s_up[d + e]) x[e] += INFINITY;
-          if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
+          for (int e = 0; e < 4; ++e) {
+            if (last[i] >= s_up[d + e]) x[e] += INFINITY;
+            if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
+          }
         }
       }
       if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part_o + to * a.D + d) = x;
