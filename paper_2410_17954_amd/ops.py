@@ -742,7 +742,7 @@ def _one_device(stream, *ts):
     """Every given tensor contiguous, on one GPU: a context in which that is the
     current device and `stream`, if there is one, the current stream, so that what
     the call allocates or fills belongs to the stream that it goes to."""
-    dev = -1
+    dev = None                         # a tensor of the host is -1
     for t in ts:
         if t is None:
             continue
@@ -750,7 +750,7 @@ def _one_device(stream, *ts):
         if d != dev:
             if d < 0:
                 raise ValueError("every tensor must be on the GPU")
-            if dev >= 0:
+            if dev is not None:
                 raise ValueError("every tensor must be on the same GPU")
             dev = d
         if not t.is_contiguous():
@@ -1008,13 +1008,13 @@ def _checked(stream, strided, *specs):
     """_one_device and _want in one pass, for calls whose time is the host's. specs:
     (name, tensor or None, shape or None, dtype or None), contiguous; strided: tensors
     whose layout has been checked."""
-    dev = -1
+    dev = None                         # a tensor of the host is -1
     for t in strided:
         d = t.get_device()
         if d != dev:
             if d < 0:
                 raise ValueError("every tensor must be on the GPU")
-            if dev >= 0:
+            if dev is not None:
                 raise ValueError("every tensor must be on the same GPU")
             dev = d
     for name, t, shape, dtype in specs:
@@ -1026,7 +1026,7 @@ def _checked(stream, strided, *specs):
         if d != dev:
             if d < 0:
                 raise ValueError("every tensor must be on the GPU")
-            if dev >= 0:
+            if dev is not None:
                 raise ValueError("every tensor must be on the same GPU")
             dev = d
         if not t.is_contiguous():

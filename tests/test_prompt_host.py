@@ -8,6 +8,7 @@ import re
 
 import numpy as np
 import pytest
+import torch
 
 import oracle
 from paper_2410_17954_amd import ops
@@ -263,3 +264,23 @@ def test_prompt_kernels_spill_nothing():
                 for n, k in kernels.items() if name in n}
         assert mine, name
         assert not {n: v for n, v in mine.items() if any(v)}
+
+
+def test_tensors_of_the_host_are_refused(lib):
+    """In the first place too: what a check of one device compares the others with."""
+    x, q = torch.zeros((2, 4, 64)), torch.zeros((2, 4, 64))
+    i = lambda *v: torch.tensor(v, dtype=torch.int32)
+    cache = tuple(torch.zeros((1, 8, 4, w), dtype=torch.uint8) for w in (32, 2, 32, 2))
+    k4 = torch.zeros((2, 3, 4, 64))
+    w = torch.zeros((4, 8, 16))
+    for call in (lambda: ops.prompt_attention(q, x, x), lambda: ops.kv4_store(x, x, cache),
+                 lambda: ops.kv4_load(cache), lambda: ops.kv4_load(cache, k=x, v=x),
+                 lambda: ops.kv4_attention(x[:1], cache),
+                 lambda: ops.token_logprobs(x[0], i(1, 2, 3, 4).view(4, 1)),
+                 lambda: ops.prefix_attention(q, k4, k4),
+                 lambda: ops.layer_decode(torch.zeros((2, 16)), torch.zeros((4, 16)), w, w,
+                                          w.transpose(1, 2).contiguous(), 2),
+                 lambda: ops.beam_select(torch.zeros((1, 2, 9)), torch.zeros((1, 2))),
+                 lambda: ops.beam_reorder([torch.zeros((1, 2, 3, 8))], i(0, 1).view(1, 2))):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call()
