@@ -259,6 +259,7 @@ lp_kernel(LpArgs a) {
   };
   // a wave reads again what its threads of a maximum from T on had read
   for (uint64_t own = ballot(float_order(best) >= bound); own; own &= own - 1) {
+    if (__builtin_amdgcn_readfirstlane(*static_cast<volatile int*>(&s_count)) > kKeys) break;   // below
     const int o = wave * kWave + __ffsll((unsigned long long)own) - 1;
     for (int at = o + lane * T; at < nvec; at += kWave * T) {
       float v[VE];
@@ -273,69 +274,111 @@ lp_kernel(LpArgs a) {
     }
   }
   __syncthreads();
-  const int count = s_count;
-  if (count <= kKeys) {
-    for (int i = t; i < count; i += T) {
-      const float v = s_key[i];
-      const int32_t id = s_idx[i];
-      int r = 0;
-#pragma unroll 4
-      for (int o = 0; o < count; ++o)
-        r += (s_key[o] > v) | ((s_key[o] == v) & (s_idx[o] < id));
-      if (r < a.n_top) {
-        out_idx[r] = id;
-        out_val[r] = logprob(v);
+  int count = s_count;
+  if (count > kKeys) {
+    // That many equal ones at the bound (a mask of the lowest number that leaves fewer
+    // than n_top): the n_top-th largest exactly, eight bits of its order at a time from
+    // how often each continuation of them occurs, then what is above it and the first
+    // of its equals (64 rows of 128000, three left, 20 places: 105 us; one pass over the
+    // row a place took 708).
+    int32_t* const often = s_idx;                // of the 256 continuations
+    const uint32_t low = float_order(-FLT_MAX);
+    uint32_t nth = 0, bits = 0;
+    int left = a.n_top;                          // equals of nth, in the bits so far, to take
+    auto some = [&](float (&v)[4], int i) {      // loads that do not wait for each other
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = i + u * T < V ? LV::one(z + i + u * T) : -INFINITY;
+    };
+    for (int shift = 24; shift >= (VE == 8 ? 16 : 0); shift -= 8) {   // bf16: the rest is its sign
+      __syncthreads();
+      for (int i = t; i < 256; i += T) often[i] = 0;
+      __syncthreads();
+      for (int i0 = t; i0 - t < V; i0 += 4 * T) {
+        float v[4];
+        some(v, i0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t k = float_order(v[u]);
+          const bool in = k >= low && (k & bits) == nth;
+          const int next = (int)(k >> shift & 255u);
+          if (const uint64_t any = ballot(in)) { // the first lane's and its equals at once
+            const int first = __ffsll((unsigned long long)any) - 1;
+            const bool same = in && next == __builtin_amdgcn_readlane(next, first);
+            const uint64_t equals = ballot(same);
+            if (lane == first) atomicAdd(often + next, (int)__popcll(equals));
+            else if (in && !same) atomicAdd(often + next, 1);
+          }
+        }
       }
-    }
-    for (int j = count + t; j < a.n_top; j += T) {
-      out_idx[j] = -1;
-      out_val[j] = -INFINITY;
-    }
-    return;
-  }
-  __syncthreads();                               // s_key is rewritten below
-  // so many equal ones: the best after the one before, again and again over the row
-  float pv = INFINITY;
-  int pi = -1;
-  for (int j = 0; j < a.n_top; ++j) {
-    float bv = -INFINITY;
-    int bi = 0x7fffffff;
-    for (int i = t; i < V; i += T) {
-      const float v = LV::one(z + i);
-      if (v > -INFINITY && (v < pv || (v == pv && i > pi)) && v > bv) {
-        bv = v;
-        bi = i;
+      __syncthreads();
+      // every wave for itself, lane l the continuations 4 l .. 4 l + 3
+      int c[4], mine = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine += c[e] = often[4 * lane + e];
+      int from = mine;                           // as often from the lane's on
+      for (int d = 1; d < kWave; d <<= 1) {
+        const int more = __shfl_down(from, d, kWave);
+        if (lane + d < kWave) from += more;
       }
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-      const float ov = __shfl_xor(bv, o, kWave);
-      const int oi = __shfl_xor(bi, o, kWave);
-      if (ov > bv || (ov == bv && oi < bi)) {
-        bv = ov;
-        bi = oi;
+      const int l = 63 - __clzll((long long)ballot(from >= left));
+      left -= __builtin_amdgcn_readlane(from - mine, l);
+      int next = 4 * l + 3;
+#pragma unroll
+      for (int e = 3; e > 0; --e) {
+        const int n = __builtin_amdgcn_readlane(c[e], l);
+        if (next == 4 * l + e && left > n) {
+          left -= n;
+          --next;
+        }
       }
+      nth |= (uint32_t)next << shift;
+      bits |= 255u << shift;
     }
-    if (lane == 0) {
-      s_key[wave] = bv;
-      s_idx[wave] = bi;
+    __syncthreads();                             // s_idx and s_count are rewritten below
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    for (int i = t; i < V; i += 4 * T) {
+      float v[4];
+      some(v, i);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if ((float_order(v[u]) & bits) > nth) offer(v[u], i + u * T);
+    }
+    __shared__ int s_equals[W];
+    for (int i0 = 0; i0 < V && left > 0; i0 += T) {
+      const int i = i0 + t;
+      const float v = i < V ? LV::one(z + i) : -INFINITY;
+      const bool in = (float_order(v) & bits) == nth;
+      const uint64_t equals = ballot(in);
+      if (lane == 0) s_equals[wave] = (int)__popcll(equals);
+      __syncthreads();
+      int before = (int)__popcll(equals & ((1ull << lane) - 1)), all = 0;
+      for (int w = 0; w < W; ++w) {
+        if (w < wave) before += s_equals[w];
+        all += s_equals[w];
+      }
+      if (in && before < left) offer(v, i);
+      left -= all;
+      __syncthreads();                           // s_equals is rewritten next
     }
     __syncthreads();
-    bv = s_key[0];
-    bi = s_idx[0];
-#pragma unroll
-    for (int w = 1; w < W; ++w)
-      if (s_key[w] > bv || (s_key[w] == bv && s_idx[w] < bi)) {
-        bv = s_key[w];
-        bi = s_idx[w];
-      }
-    if (t == 0) {
-      const bool got = bi != 0x7fffffff;
-      out_idx[j] = got ? bi : -1;
-      out_val[j] = got ? logprob(bv) : -INFINITY;
+    count = s_count;                             // n_top
+  }
+  for (int i = t; i < count; i += T) {
+    const float v = s_key[i];
+    const int32_t id = s_idx[i];
+    int r = 0;
+#pragma unroll 4
+    for (int o = 0; o < count; ++o)
+      r += (s_key[o] > v) | ((s_key[o] == v) & (s_idx[o] < id));
+    if (r < a.n_top) {
+      out_idx[r] = id;
+      out_val[r] = logprob(v);
     }
-    pv = bv;
-    pi = bi;
-    __syncthreads();                             // s_key is rewritten next
+  }
+  for (int j = count + t; j < a.n_top; j += T) {
+    out_idx[j] = -1;
+    out_val[j] = -INFINITY;
   }
 }
 
