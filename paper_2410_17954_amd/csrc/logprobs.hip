@@ -259,7 +259,8 @@ lp_kernel(LpArgs a) {
   };
   // a wave reads again what its threads of a maximum from T on had read
   for (uint64_t own = ballot(float_order(best) >= bound); own; own &= own - 1) {
-    if (__builtin_amdgcn_readfirstlane(*static_cast<volatile int*>(&s_count)) > kKeys) break;   // below
+    // too many already: the passes below take over
+    if (__builtin_amdgcn_readfirstlane(*static_cast<volatile int*>(&s_count)) > kKeys) break;
     const int o = wave * kWave + __ffsll((unsigned long long)own) - 1;
     for (int at = o + lane * T; at < nvec; at += kWave * T) {
       float v[VE];

@@ -86,6 +86,22 @@ def test_ties_and_order(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R", [6, 300])
+def test_more_near_the_bound_than_places(R, dtype):
+    g = np.random.default_rng(R)
+    V = 9001
+    z = np.zeros((R, V))
+    z[0] = 1 + g.integers(0, 4096, V) * 2.0 ** -23   # apart in their last bits only
+    z[1] = -1 - g.integers(0, 300, V) * 2.0 ** -23
+    z[2] = g.integers(0, 40, V) * 2.0 ** -149        # float32's least numbers
+    z[3], z[3, [7, V - 1, 4000]] = MIN[dtype], [1.0, 3.0, 2.0]
+    z[4], z[4, V - 2000:], z[4, V - 1000] = -np.inf, 5.0, 6.0
+    z[5], z[5, ::5] = MIN[dtype], 0.25
+    for n in (1, 3, 4, 64):
+        _check(_cast(z, dtype), g.integers(0, V, (R, 1)), n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [60, 3000, 33000])
 def test_masks_infinities_and_nan(V, dtype):
     g = np.random.default_rng(V)
