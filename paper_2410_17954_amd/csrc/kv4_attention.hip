@@ -62,14 +62,16 @@ __device__ __forceinline__ u32x4_t eight_bf16(uint32_t w, float scale) {
   return x;
 }
 
-// x as a sum of NS bf16 numbers: cut, not rounded, so that three hold all 24 bits.
-template <int NS>
+// x as a sum of NS bf16 numbers: cut, not rounded, so that three hold all 24 bits. INF: x
+// may be infinite, which is all in the first part (infinity less itself is a NaN). A NaN
+// is one in some part.
+template <int NS, bool INF>
 __device__ __forceinline__ void cut(float x, uint16_t (&part)[NS]) {
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
     const uint32_t top = __float_as_uint(x) & 0xffff0000u;
     part[n] = (uint16_t)(top >> 16);
-    x -= __uint_as_float(top);
+    x = INF && fabsf(x) == INFINITY ? 0.f : x - __uint_as_float(top);
   }
 }
 
@@ -220,7 +222,7 @@ struct KaCore {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             uint16_t part[NS];
-            cut<NS>(ps[e / 4][e % 4], part);
+            cut<NS, false>(ps[e / 4][e % 4], part);
 #pragma unroll
             for (int n = 0; n < NS; ++n) x[n][e] = part[n];
           }
@@ -308,8 +310,8 @@ ka_kernel(KaArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint16_t p0[C::NS], p1[C::NS];
-        cut<C::NS>(__uint_as_float(x[j / 2][2 * (j % 2)]), p0);
-        cut<C::NS>(__uint_as_float(x[j / 2][2 * (j % 2) + 1]), p1);
+        cut<C::NS, true>(__uint_as_float(x[j / 2][2 * (j % 2)]), p0);
+        cut<C::NS, true>(__uint_as_float(x[j / 2][2 * (j % 2) + 1]), p1);
 #pragma unroll
         for (int n = 0; n < C::NS; ++n) q[n][t][j] = (uint32_t)p0[n] | (uint32_t)p1[n] << 16;
       }
