@@ -62,16 +62,15 @@ __device__ __forceinline__ u32x4_t eight_bf16(uint32_t w, float scale) {
   return x;
 }
 
-// x as a sum of NS bf16 numbers: cut, not rounded, so that three hold all 24 bits. INF: x
-// may be infinite, which is all in the first part (infinity less itself is a NaN). A NaN
-// is one in some part.
-template <int NS, bool INF>
+// x as a sum of NS bf16 numbers: cut, not rounded, so that three hold all 24 bits. Of an
+// infinity the first part is one and the others are NaN.
+template <int NS>
 __device__ __forceinline__ void cut(float x, uint16_t (&part)[NS]) {
 #pragma unroll
   for (int n = 0; n < NS; ++n) {
     const uint32_t top = __float_as_uint(x) & 0xffff0000u;
     part[n] = (uint16_t)(top >> 16);
-    x = INF && fabsf(x) == INFINITY ? 0.f : x - __uint_as_float(top);
+    x -= __uint_as_float(top);
   }
 }
 
@@ -222,7 +221,7 @@ struct KaCore {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             uint16_t part[NS];
-            cut<NS, false>(ps[e / 4][e % 4], part);
+            cut<NS>(ps[e / 4][e % 4], part);
 #pragma unroll
             for (int n = 0; n < NS; ++n) x[n][e] = part[n];
           }
@@ -293,6 +292,7 @@ ka_kernel(KaArgs a) {
             min(hi - key, KEYS), off[x], a);
   };
   u32x4_t q[C::NS][C::WN];
+  float q_top = 0.f;
 #pragma unroll
   for (int t = 0; t < C::WN; ++t) {
     const int d = q4 * (DP / 4) + 8 * t;
@@ -309,12 +309,30 @@ ka_kernel(KaArgs a) {
           x[i] = (reinterpret_cast<const u32x4_t*>(src)[i] & a.keep) ^ a.flip;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        const float x0 = __uint_as_float(x[j / 2][2 * (j % 2)]);
+        const float x1 = __uint_as_float(x[j / 2][2 * (j % 2) + 1]);
         uint16_t p0[C::NS], p1[C::NS];
-        cut<C::NS, true>(__uint_as_float(x[j / 2][2 * (j % 2)]), p0);
-        cut<C::NS, true>(__uint_as_float(x[j / 2][2 * (j % 2) + 1]), p1);
+        cut<C::NS>(x0, p0);
+        cut<C::NS>(x1, p1);
+        q_top = fmaxf(q_top, fmaxf(fabsf(x0), fabsf(x1)));
 #pragma unroll
         for (int n = 0; n < C::NS; ++n) q[n][t][j] = (uint32_t)p0[n] | (uint32_t)p1[n] << 16;
       }
+    }
+  }
+  // All of an infinite channel is in its first part. Looked for once a lane: a selection
+  // for every channel took 0.3 us of a call.
+  if (!C::BF16 && q_top == INFINITY) {
+#pragma unroll
+    for (int t = 0; t < C::WN; ++t) {
+      const int d = q4 * (DP / 4) + 8 * t;
+      if (d >= a.D) continue;
+      const float* const src = static_cast<const float*>(a.q) + at * a.D + d;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (fabsf(src[j]) == INFINITY)
+#pragma unroll
+          for (int n = 1; n < C::NS; ++n) q[n][t][j / 2] &= j % 2 ? 0xffffu : 0xffff0000u;
     }
   }
   f32x4_t o[1][DT];
