@@ -36,7 +36,10 @@ extern "C" {
  * A query without any key (i < n - m), or whose scores are all -inf: out 0, lse
  * -inf. What later tokens hold does not reach earlier ones, be it NaN. Float32
  * scores, statistics and accumulation; bf16: the softmax numerators are rounded to
- * bf16 for the second product, their sum is not. Results do not depend on scheduling.
+ * bf16 for the second product, their sum is not. Sums of values are held with weights
+ * of at most 1 and divided by the weights' sum at the end: results are finite where the
+ * sum of |v| over a query's keys is below 3.4e38; terms below 2^-118 may count as 0.
+ * Results do not depend on scheduling.
  *
  * q    [N, Hq, D] dtype, tokens q_stride elements apart (at least Hq * D)
  * k, v [M, Hkv, D] dtype, tokens k_stride, v_stride elements apart (at least
@@ -110,7 +113,8 @@ int moe_kv4_load(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t*
  * A row without any key, or whose scores are all -inf: out 0, lse -inf. Float32
  * scores, statistics and accumulation; with float32 q products are of 24 bits, with
  * bf16 the softmax numerators are rounded to bf16 for the second product, their sum
- * is not. Results do not depend on scheduling. lse joins the result with that over
+ * is not. Large and small values as for moe_prompt_attention: one key of 6 * 2^125 is
+ * held. Results do not depend on scheduling. lse joins the result with that over
  * other keys (moe_prefix_attention).
  *
  * q, out     [R, Hq, D] dtype; lse [R, Hq] float32 or NULL

@@ -363,7 +363,7 @@ ka_kernel(KaArgs a) {
         for (int e = 0; e < 4; ++e)
           if (16 * q4 + 4 * kt + e >= keys) s[0][kt][e] = -INFINITY;
     }
-    softmax_step(s, m_run, l_run, o, a.scale2);
+    softmax_step<Tv>(s, m_run, l_run, o, a.scale2);
     if (one) wait_loads<G>();
     else wait_loads<0>();
     C::units(units, vc + C::kCodes);

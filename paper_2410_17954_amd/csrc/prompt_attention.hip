@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
           for (int e = 0; e < 4; ++e)
             if (key + 16 * kt + 4 * q4 + e > last[i]) s[i][kt][e] = -INFINITY;
     }
-    softmax_step(s, m_run, l_run, o, a.scale2);
+    softmax_step<Tv>(s, m_run, l_run, o, a.scale2);
     C::values(o, s, tk + C::kTile);
   };
   // as many turns for every group: they meet at the barriers

@@ -50,3 +50,50 @@ def test_infinite_queries_over_a_cache_of_4_bits(D, S, dtype):
     cache[3][:, ::5] = 255                           # whatever the values hold
     out, lse = ops.kv4_attention(q, cache, scale=0.1)
     assert (out[0, 0] == 0).all() and lse[0, 0] == -INF and torch.isnan(out[0, 3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hkv,R", [(1, 512), (4, 512), (2, 3)])
+def test_largest_values_of_a_cache_of_4_bits(Hkv, R, dtype):
+    """One key of values up to 6 * 2^125 whose score is above those of the tiles before
+    it, by less than a reference is raised for: results are finite."""
+    g = np.random.default_rng(R)
+    S, D, at = 1000, 64, 700
+    k, v = (to_dev(draw(g, "f32", S, Hkv, D, std=s)) for s in (0.1, 1.0))
+    k[:, :, 0], k[at, :, 0] = 0.0, 6.0
+    v[at] = 0.0
+    v[at, :, ::3], v[at, :, 33] = 6 * 2.0 ** 125, -2.0 ** 124
+    cache, (kk, vv) = _kv4(k, v)
+    assert np.abs(vv).max() == 6 * 2.0 ** 125 and (vv[at] == 0).any()
+    q = draw(g, dtype, R, 2 * Hkv, D, std=0.1)
+    t = to_dev(q)
+    t[:, :, 0] = 0.85                                # 5 above the others: 2^7.3
+    rows = torch.zeros(R, dtype=torch.int32, device=DEV)
+    out, lse = ops.kv4_attention(t, cache, cache_row=rows, scale=1.0)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    for r in (0, R - 1):
+        for h in range(2 * Hkv):
+            x = vals(t)[r, h]
+            ref, rl = oracle.prompt.softmax_rows(kk[:, h // 2] @ x, vv[:, h // 2])
+            check_row(vals(out)[r, h], to_host(lse)[r, h], ref, rl, x, kk[:, h // 2], vv[:, h // 2],
+                      1.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,D,n,m", [(4, 64, 700, 700), (2, 128, 5, 900), (64, 64, 600, 600)])
+def test_largest_values_of_a_prompt(Hq, D, n, m, dtype):
+    g = np.random.default_rng(n + D)
+    q, k = (to_dev(draw(g, dtype, r, h, D, std=0.1)) for r, h in ((n, Hq), (m, Hq // 2)))
+    v = to_dev(draw(g, dtype, m, Hq // 2, D))
+    at = m // 2 + 3
+    q[:, :, 0], k[:, :, 0], k[at, :, 0] = 1.0, 0.0, 5.0
+    v[at, :, ::3] = 2.5e38                           # the sum over all keys stays a float32
+    out, lse = ops.prompt_attention(q, k, v, scale=1.0)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    first = max(0, at - (m - n))
+    for r in {0, max(0, first - 1), first, n // 2, n - 1}:
+        for h in (0, Hq - 1):
+            keys = slice(0, m - n + r + 1)
+            kk, vv, x = vals(k)[keys, h // 2], vals(v)[keys, h // 2], vals(q)[r, h]
+            ref, rl = oracle.prompt.softmax_rows(kk @ x, vv)
+            check_row(vals(out)[r, h], to_host(lse)[r, h], ref, rl, x, kk, vv, 1.0, dtype)
