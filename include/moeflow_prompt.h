@@ -148,8 +148,12 @@ int moe_kv4_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, int32
  * places hold -1 and -inf. A row of nothing but -inf: logprobs -inf, entropy 0. A row
  * with a NaN or +inf: logprobs (of tokens in 0..V-1) and entropy NaN, top_tokens -1,
  * top_logprobs -inf.
- * Numerics: float32 exponentials of differences to the row's maximum, summed in
- * float64 beyond 32 of them; results rounded to float32 once.
+ * Numerics: float32 exponentials of differences to a reference within 8 of the maximum
+ * of what it stands for, summed in float64 beyond 32 of them, the best logit's terms
+ * apart where they are most of the sum. A log-probability is off by at most 2^-15 of the
+ * best token's own, the entropy by at most 2^-13 of itself, beside the rounding to
+ * float32: no log-probability is above 0, no entropy below, and both are 0 where one
+ * token has all.
  *
  * logits  [R, V] dtype, rows `stride` elements apart (at least V), any
  *         element-aligned address

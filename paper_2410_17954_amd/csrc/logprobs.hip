@@ -4,9 +4,14 @@
 // in turn, the next ones in flight, and each keeps a reference ref, s = sum e^(z - ref)
 // and h = sum e^(z - ref) (z - ref) of what it saw:
 //   ln sum e^z = M + ln S,   entropy = ln S - H / S
-// with S and H the threads' sums brought to the largest reference M. A reference is
+// with S and H the threads' sums brought to the best logit M. A reference is
 // raised only where a logit exceeds it by more than kSlack, so almost never after the
-// first ones.
+// first ones. Exponentials and short sums are of float32: S is off by up to 2^-17 of
+// itself. Where S is below 2 that is much beside ln S, which is next to 0: the threads
+// that hold the best logit then have their logits read again and the others' terms summed
+// apart from it, S = C + rest with C the (one or two) terms that are 1. So what is next to
+// 0 is off by a part of itself, and with one token left 0 (0.4 us of a row of 32000, 8.3;
+// to count the best while the row is read took 2 of 8.3, 13 of 104 for 2000 x 128000).
 // Best alternatives need no second pass over the row: of kGroups groups of threads the
 // n-th largest of their maxima, cut to some leading bits, is a bound T that n logits
 // reach, and only threads whose own maximum reaches T hold more of them, about n. A
@@ -80,11 +85,25 @@ __device__ __forceinline__ double lp_exp(double d) {
   return ldexp((double)__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
 }
 
-// ln x of a positive number, off by 2^-24 (|ln of its mantissa| is below 0.7); NaN of NaN.
-__device__ __forceinline__ double lp_log(double x) {
+// ln(1 + x), x >= 0, off by 2^-33 of itself: with 1 + x = 2^e (1 + f), 1 + f within a
+// factor sqrt(2) of 1 (f = x where e is 0, however small), ln(1 + f) = 2 artanh(f / (2 + f))
+// by its series. NaN of NaN.
+__device__ __forceinline__ double lp_log1p(double x) {
   int e;
-  const float f = (float)frexp(x, &e);
-  return (double)e * 0.6931471805599453 + (double)(__builtin_amdgcn_logf(f) * 0.6931471805599453f);
+  double m = frexp(1.0 + x, &e);
+  if (m < 0.7071067811865476) {
+    m *= 2.0;
+    --e;
+  }
+  const double f = e == 0 ? x : m - 1.0, y = 2.0 + f;
+  double c = __builtin_amdgcn_rcp(y);            // and a step of Newton's
+  c = fma(c, fma(-y, c, 1.0), c);
+  const double r = f * c, z = r * r;
+  double p = fma(z, 1.0 / 11, 1.0 / 9);
+  p = fma(z, p, 1.0 / 7);
+  p = fma(z, p, 1.0 / 5);
+  p = fma(z, p, 1.0 / 3);
+  return fma((double)e, 0.6931471805599453, 2.0 * fma(r * z, p, r));
 }
 
 // Brings sums to a reference at least as large. No logits: ref -inf, sums 0.
@@ -98,6 +117,36 @@ __device__ __forceinline__ void lp_raise(LpSum& x, float to) {
   x.ref = to;
 }
 
+// Over the wave: rows of 16 lanes by DPP, then the four rows.
+__device__ __forceinline__ double lp_lane(double v, int l) {
+  const uint64_t b = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, l);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), l);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+template <typename T>
+__device__ __forceinline__ T lp_row_sum(T v) {
+  v += dpp<0xB1>(v);
+  v += dpp<0x4E>(v);
+  v += dpp<0x141>(v);
+  return v + dpp<0x140>(v);
+}
+__device__ __forceinline__ double lp_wave_sum(double v) {
+  v = lp_row_sum(v);
+  return (lp_lane(v, 0) + lp_lane(v, 16)) + (lp_lane(v, 32) + lp_lane(v, 48));
+}
+__device__ __forceinline__ float lp_row_max(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  v = fmaxf(v, dpp<0x4E>(v));
+  v = fmaxf(v, dpp<0x141>(v));
+  return fmaxf(v, dpp<0x140>(v));
+}
+__device__ __forceinline__ float lp_wave_max(float v) {
+  v = lp_row_max(v);
+  auto at = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return fmaxf(fmaxf(at(0), at(16)), fmaxf(at(32), at(48)));
+}
+
 // T threads, U 16-byte loads of each in flight beside the ones in work.
 template <typename Tv, int T, int U, bool NT>
 __global__ void __launch_bounds__(T)
@@ -108,6 +157,7 @@ lp_kernel(LpArgs a) {
   constexpr int PART = U * VE < 32 ? U * VE : 32;
   __shared__ float s_ref[W];
   __shared__ double s_s[W], s_h[W];
+  __shared__ int s_ones[W];
   __shared__ float s_max[kGroups];
   __shared__ int s_count;
   __shared__ float s_key[kKeys];
@@ -180,16 +230,18 @@ lp_kernel(LpArgs a) {
   }
 
   // the waves' sums and the groups' maxima
-  float ref = x.ref;
-  for (int o = 32; o > 0; o >>= 1) ref = fmaxf(ref, __shfl_xor(ref, o, kWave));
+  const float ref = lp_wave_max(best);
   lp_raise(x, ref);
-  x.s = wave_sum(x.s);
-  x.h = wave_sum(x.h);
-  if (lane == 0) {
-    s_ref[wave] = ref;
-    s_s[wave] = x.s;
-    s_h[wave] = x.h;
-  }
+  auto publish = [&](double s, double h) {
+    s = lp_wave_sum(s);
+    h = lp_wave_sum(h);
+    if (lane == 0) {
+      s_s[wave] = s;
+      s_h[wave] = h;
+    }
+  };
+  if (lane == 0) s_ref[wave] = ref;
+  publish(x.s, x.h);
   float gmax = best;                             // a group is T / kGroups neighbours
   if (T > kGroups) gmax = fmaxf(gmax, dpp<0xB1>(gmax));
   if (T > 2 * kGroups) gmax = fmaxf(gmax, dpp<0x4E>(gmax));
@@ -197,25 +249,67 @@ lp_kernel(LpArgs a) {
   __syncthreads();
 
   // the row's: every wave for itself, lane w % 16 the sums of wave w
-  float M = s_ref[lane % 16 % W];
-  LpSum y = {M, s_s[lane % 16 % W], s_h[lane % 16 % W]};
-  if (lane % 16 >= W) y.s = y.h = 0.0;
-  M = fmaxf(M, dpp<0xB1>(M));
-  M = fmaxf(M, dpp<0x4E>(M));
-  M = fmaxf(M, dpp<0x141>(M));
-  M = fmaxf(M, dpp<0x140>(M));
-  lp_raise(y, M);
-  double S = y.s, H = y.h;
-  auto row_sum = [](double v) {
-    v += dpp<0xB1>(v);
-    v += dpp<0x4E>(v);
-    v += dpp<0x141>(v);
-    return v + dpp<0x140>(v);
+  const int of = lane % 16 % W;
+  const bool one = lane % 16 < W;
+  const float w_ref = s_ref[of];
+  float M = lp_row_max(w_ref);
+  const double w_d = w_ref == M ? 0.0 : (double)w_ref - (double)M;
+  const double w_f = one ? lp_exp(w_d) : 0.0;    // 0 far below: whatever the difference
+  double S, H;
+  auto sum_waves = [&]() {
+    const double s = s_s[of], h = s_h[of];
+    const bool some = w_f > 0.0 || s != s;
+    S = lp_row_sum(w_f * s);
+    H = lp_row_sum(some ? w_f * (h + w_d * s) : 0.0);
   };
-  S = row_sum(S);
-  H = row_sum(H);
+  sum_waves();
   const bool none = M == -INFINITY && S == 0.0;
-  const double lnS = none ? 0.0 : lp_log(S);     // NaN of a row with a NaN or +inf
+  double lnS = 0.0;
+  if (!(S < 2.0)) {
+    lnS = lp_log1p(S - 1.0);                     // NaN of a row with a NaN or +inf
+  } else if (!none) {                            // the same in every wave
+    __syncthreads();                             // s_s and s_h are rewritten below
+    int ones = 0;
+    const uint64_t owners = ballot(best == M);
+    if (owners) {                                // this wave's reference is M
+      double s = best == M ? 0.0 : x.s, h = best == M ? 0.0 : x.h;
+      auto others = [&](const float* v, int n) {
+        float s32 = 0.f, h32 = 0.f;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const float d = v[i] - M;
+          const float e = v[i] == M ? 0.f : __builtin_amdgcn_exp2f(d * kLog2e);
+          ones += v[i] == M;
+          s32 += e;
+          h32 = fmaf(e, fmaxf(d, -200.f), h32);
+        }
+        s += (double)s32;
+        h += (double)h32;
+      };
+#pragma unroll 1
+      for (uint64_t own = owners; own; own &= own - 1) {
+        const int o = wave * kWave + __ffsll((unsigned long long)own) - 1;
+#pragma unroll 1
+        for (int at = o + lane * T; at < nvec; at += kWave * T) {
+          float v[VE];
+          LV::unpack(*reinterpret_cast<const Bytes16*>(z + (int64_t)at * VE), v);
+          others(v, VE);
+        }
+        if (lane == 0 && o < rest) {
+          const float v = LV::one(z + nvec * VE + o);
+          others(&v, 1);
+        }
+      }
+      publish(s, h);
+      ones = (int)lp_wave_sum((double)ones);
+    }
+    if (lane == 0) s_ones[wave] = ones;
+    __syncthreads();
+    sum_waves();
+    const int C = lp_row_sum(one ? s_ones[of] : 0);
+    lnS = lp_log1p((double)(C - 1) + S);
+    S += (double)C;
+  }
   if (none) M = 0.f;
   if (t == 0 && a.entropy) a.entropy[row] = none ? 0.f : (float)(lnS - H / S);
   // the difference to the maximum first: beside a mask's lowest number ln S is lost

@@ -97,3 +97,93 @@ def test_largest_values_of_a_prompt(Hq, D, n, m, dtype):
             kk, vv, x = vals(k)[keys, h // 2], vals(v)[keys, h // 2], vals(q)[r, h]
             ref, rl = oracle.prompt.softmax_rows(kk @ x, vv)
             check_row(vals(out)[r, h], to_host(lse)[r, h], ref, rl, x, kk, vv, 1.0, dtype)
+
+
+def _check_logprobs(x, tokens, n_top, dtype):
+    """Rows of numbers and -inf (float64 of the exact logits). With d = max - z, u =
+    2^-24, the exponential of a logit is off by
+    * 2.25 max(d, 8) u: its difference to a reference at most 8 below it or d above it is
+      rounded, the factor log2 e, and their product;
+    * 2 u of the exponential itself, 3 u at each change of reference (d / 8 in a thread,
+      of the thread, the wave and the block), 32 u of a float32 sum of 32 terms,
+    relative to p = e^-d / sum. Where the sum is below 2 terms of the maximum (d = 0) are
+    exact, a sum apart: |d ln sum| <= sum of p times those over the others, and what is too
+    small for a float32. The entropy's second sum has them times |z - ref| + |ref - max| <=
+    max(d, 8) + d + 8 and 2 u d more. Every result is rounded once; the reference, float64
+    sums and a logarithm of numbers next to 1, is off by some 2^-51."""
+    u = 2.0 ** -24
+    z = torch.from_numpy(x).to(_dtype(dtype)).to(DEV)
+    x = vals(z)
+    rl, re, rt, rtl = oracle.token_logprobs(x, tokens, n_top)
+    d = x.max(1, keepdims=True) - x
+    p = np.exp(-d)
+    p /= p.sum(1, keepdims=True)
+    fin = np.where(np.isfinite(d), d, 0.0)
+    exact = np.exp(-d).sum(1, keepdims=True) < 1.99
+    rest = np.where((d > 0) & np.isfinite(d) | ~exact & (d == 0), p, 0.0)
+    rel = u * (2.25 * np.maximum(fin, 8) + 2 + 3 * (fin / 8 + 3) + 32) * 1.01
+    e_ln = (rest * rel).sum(1) + x.shape[1] * 2.0 ** -126 + 2.0 ** -50
+    e_h = (rest * (rel * (np.maximum(fin, 8) + fin + 8) + 2 * u * fin)).sum(1)
+    lp, en, tt, tl = (to_host(a).astype(np.float64) for a in ops.token_logprobs(
+        z, to_dev(tokens.astype(np.int32)), n_top))
+    for got, ref, bound in ((lp, rl, e_ln[:, None]), (tl, rtl, e_ln[:, None]),
+                            (en, re, e_ln * (1 + (rest * fin).sum(1)) + e_h)):
+        ok = np.broadcast_to(np.isfinite(ref), ref.shape)
+        assert np.array_equal(np.isfinite(got), ok)
+        bound = np.broadcast_to(bound, ref.shape)[ok] + u * np.abs(ref[ok])
+        err = np.abs(got[ok] - ref[ok])
+        assert (err <= bound).all(), (err - bound).max()
+    assert np.array_equal(tt, rt)
+    assert not (lp > 0).any() and not (tl > 0).any() and not (en < 0).any()
+    return lp, en, tl
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(1, 1), (3, 1), (4, 2), (4, 100), (300, 257), (5, 2049), (2, 32000),
+                                 (300, 33001), (1, 128000)])
+def test_one_token_has_all(R, V, dtype):
+    """One logit left, or one that is far above: its log-probability and the entropy
+    are 0, not next to it."""
+    g = np.random.default_rng(R + V)
+    at = g.integers(0, V, R)
+    for low in (-np.inf, -3.3e38, -1e4):
+        x = np.full((R, V), low)
+        x[np.arange(R), at] = g.choice([-5.0, 0.0, 1.0, 77.0], R)
+        lp, en, tl = _check_logprobs(x, at[:, None], 1, dtype)
+        assert (lp == 0).all() and (en == 0).all() and (tl == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(4, 60), (6, 3001), (5, 32000), (300, 32000), (3, 128000)])
+def test_confident_rows(R, V, dtype):
+    """The best of a row some 8 to 30 above the others: its log-probability is -(1 - p),
+    with as many right digits as that has; wherever the best one stands."""
+    g = np.random.default_rng(V)
+    for above in (8.0, 12.5, 17.25, 30.0):
+        x = g.standard_normal((R, V)) - 1.0
+        at = g.integers(0, V, R)
+        at[:3] = 0, V - 1, V // 2
+        x[np.arange(R), at] = above
+        x[0, V // 3] = above - 0.5                   # a close second
+        lp, _, _ = _check_logprobs(x, np.stack([at, (at + 1) % V], 1), 3, dtype)
+    assert (lp[1:, 0] > -1e-5).all() and (lp[1:, 0] < 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R", [6, 300])
+def test_references_behind_the_maximum(R, dtype):
+    """Rows that rise, by steps below and above what a reference is raised for; equal
+    maxima; equal rows."""
+    g = np.random.default_rng(R)
+    V = 40001
+    at = np.arange(V)
+    x = g.standard_normal((R, V))
+    x[0] += 7.5 * (at >= 0.9 * V)
+    x[1] += 20.0 * at / V
+    x[2] += 100.0 * at / V
+    x[3, V - 1], x[3, 5] = 12.0, 12.0
+    x[4] = 1.5
+    x[5, V - 700:] = 12.5
+    for j in range(6, R):
+        x[j] += (j % 17) * (at >= V - 1 - 37 * j)
+    _check_logprobs(x, g.integers(0, V, (R, 2)), 4, dtype)
