@@ -34,7 +34,9 @@ extern "C" {
  *   s_j       = scale * q[i, h] . k[j, h / (Hq / Hkv)]
  *   out[i, h] = sum_j softmax(s)_j v[j, h / (Hq / Hkv)],  lse[i, h] = ln sum_j exp s_j
  * A query without any key (i < n - m), or whose scores are all -inf: out 0, lse
- * -inf. What later tokens hold does not reach earlier ones, be it NaN. Float32
+ * -inf. What later tokens hold does not reach earlier ones, be it NaN. An infinite
+ * value of a key that a query attends to counts whatever the key's weight, also 0:
+ * that dimension of out is the infinity, or NaN of a NaN or of both signs. Float32
  * scores, statistics and accumulation; bf16: the softmax numerators are rounded to
  * bf16 for the second product, their sum is not. Sums of values are held with weights
  * of at most 1 and divided by the weights' sum at the end: results are finite where the

@@ -168,7 +168,8 @@ attention_join_kernel(JoinArgs a, int tpr_shift, int sg_shift) {
       }
       l = fmaf(ml.y, f, l);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(po[e], f, o[e]);
+      for (int e = 0; e < 4; ++e)                // an infinity counts whatever its weight
+        o[e] = fmaf(po[e], fabsf(po[e]) == INFINITY ? 1.f : f, o[e]);
     }
   }
   for (int n = sg >> 1; n > 0; n >>= 1) {

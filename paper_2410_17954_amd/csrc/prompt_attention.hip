@@ -32,6 +32,7 @@ namespace moe {
 namespace {
 
 constexpr uint32_t kPastEnd = 0xfffffff0u;       // no buffer here is as long
+constexpr int kLook = 2;                         // of s_odd: values are to be looked at again
 
 struct PrArgs {
   const void *q, *k, *v;
@@ -244,38 +245,67 @@ struct PrCore {
       }
     }
   }
-  // Values that are no numbers, in a tile that some query does not see as a whole:
-  // 0 times them would be NaN. Of the chunks that this wave loaded they become 0, and
-  // for every dimension the first key of +inf or NaN and of -inf or NaN is kept: a
-  // query that sees it gets the infinity, or both, at the end. *any: there are such
-  // (the end of a block without them is 1 us shorter: 8 tokens 6.2 -> 5.2).
+  // For every dimension the first key whose value is +inf or NaN, and -inf or NaN: a query
+  // that sees it gets the infinity, or both, whatever the key's weight. Of eight (four)
+  // values from dimension d0 on, which become 0 in x if it is to hold no others.
+  static __device__ __forceinline__ bool is_odd(const u32x4_t& w) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      odd |= (w[e] & 0x7f800000u) == 0x7f800000u;
+      if constexpr (BF16) odd |= (w[e] & 0x7f80u) == 0x7f80u;
+    }
+    return odd;
+  }
+  template <bool CLEAR, typename T>
+  static __device__ __forceinline__ void note_odd(T* x, int d0, int key, int* up, int* down) {
+#pragma unroll 1
+    for (int e = 0; e < VE; ++e) {
+      float f;
+      if constexpr (BF16) f = bf16_to_f32(x[e]);
+      else f = x[e];
+      if (fabsf(f) < INFINITY) continue;
+      if (!(f < 0.f)) atomicMin(up + d0 + e, key);
+      if (!(f > 0.f)) atomicMin(down + d0 + e, key);
+      if constexpr (CLEAR) x[e] = 0;
+    }
+  }
+  // In a tile that some query does not see as a whole 0 times them would be NaN: those in
+  // the chunks that this wave loaded become 0. *any: there are such (the end of a block
+  // without them is 1 us shorter: 8 tokens 6.2 -> 5.2).
   static __device__ __forceinline__ void take_odd(char* tile, int key, int wave, int* up, int* down,
                                                   int* any) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int g = (wave * PIECES + p) * 64 + lane_id(), row = g / CH;
       u32x4_t* const at = reinterpret_cast<u32x4_t*>(tile) + g;
-      const u32x4_t w = *at;
-      bool odd = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        odd |= (w[e] & 0x7f800000u) == 0x7f800000u;
-        if constexpr (BF16) odd |= (w[e] & 0x7f80u) == 0x7f80u;
-      }
-      if (!odd) continue;
+      if (!is_odd(*at)) continue;
       *any = 1;
-      const int d0 = ((g % CH) ^ swz_v(row)) * VE;
-      Tv* const x = reinterpret_cast<Tv*>(at);
+      note_odd<true>(reinterpret_cast<Tv*>(at), ((g % CH) ^ swz_v(row)) * VE, key + row, up, down);
+    }
+  }
+  // Other tiles are not looked at (in all tiles it was 0.7 % of long prompts and more of
+  // short ones): theirs make O infinite or NaN, and then the block's threads look at the
+  // values of all its keys once more. To see that costs 0.1 us of a call.
+  static __device__ __forceinline__ bool finite(const f32x4_t (&o)[kMT][DT]) {
+    float top[2] = {0.f, 0.f};                   // maxima that keep a NaN, two values each time
+#pragma unroll
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          top[dt % 2] = __builtin_elementwise_maximum(top[dt % 2], fabsf(o[i][dt][e]));
+    return __builtin_elementwise_maximum(top[0], top[1]) < INFINITY;
+  }
+  static __device__ __forceinline__ void find_odd(const char* v, int64_t stride, int D, int lo, int hi,
+                                                  int threads, int* up, int* down) {
+    const int d0 = (int)threadIdx.x % CH * VE;
+    if (d0 >= D) return;
 #pragma unroll 1
-      for (int e = 0; e < VE; ++e) {
-        float f;
-        if constexpr (BF16) f = bf16_to_f32(x[e]);
-        else f = x[e];
-        if (fabsf(f) < INFINITY) continue;
-        if (!(f < 0.f)) atomicMin(up + d0 + e, key + row);
-        if (!(f > 0.f)) atomicMin(down + d0 + e, key + row);
-        x[e] = 0;
-      }
+    for (int key = lo + (int)threadIdx.x / CH; key < hi; key += threads / CH) {
+      const Tv* const from = reinterpret_cast<const Tv*>(v) + key * stride + d0;
+      if (is_odd(*reinterpret_cast<const u32x4_t*>(from))) note_odd<false>(from, d0, key, up, down);
     }
   }
 };
@@ -385,6 +415,16 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
   float l_all[kMT];
 #pragma unroll
   for (int i = 0; i < kMT; ++i) l_all[i] = quad_sum(l_run[i]);
+  // take_odd is done: every wave has passed the last tile's barrier
+  if (j.lo + BN <= b_all && !C::finite(o)) atomicOr(&s_odd, kLook);
+  bool odd;
+  auto look = [&]() {                            // after a barrier
+    const int what = __builtin_amdgcn_readfirstlane(s_odd);
+    odd = what != 0;
+    if (!(what & kLook)) return;
+    C::find_odd(j.v, a.v_stride, a.D, j.lo, j.hi, 64 * W * KS, s_up, s_down);
+    __syncthreads();
+  };
   if constexpr (KS > 1) {
 #pragma unroll
     for (int i = 0; i < kMT; ++i)
@@ -393,6 +433,7 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
         s_l[group][w_off + 16 * i + r] = l_all[i];
       }
     __syncthreads();                             // and every wave is done with its tiles
+    look();
     f32x4_t* const part = reinterpret_cast<f32x4_t*>(lds);
 #pragma unroll
     for (int i = 0; i < kMT; ++i) {
@@ -423,17 +464,18 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
           o[i][dt] += part[(((any + g * W) * kMT + i) * DT + dt) * kWave + lane];
   } else {
     __syncthreads();
+    look();
   }
   const int64_t RH = a.N * a.Hq;
-  const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
     const float l = l_all[i];
     if (w_m + 16 * i + r >= j.cols) continue;
     const int64_t to = j.split * RH + at[i];
     const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    // a split of no weight may hold infinities: its sum, of a maximum of -inf, adds 0
     if (q4 == 0) {
-      if (a.splits > 1) a.part_ml[to] = make_float2(m_run[i], l);
+      if (a.splits > 1) a.part_ml[to] = make_float2(m_run[i], odd && l == 0.f ? 1.f : l);
       else if (a.lse) a.lse[to] = lse_of(m_run[i], l);
     }
 #pragma unroll
@@ -441,14 +483,13 @@ __global__ void __launch_bounds__(64 * W * KS, 2) pr_kernel(PrArgs a) {
       const int d = 16 * dt + 4 * q4;            // D is a multiple of 8
       if (d >= a.D) continue;
       f32x4_t x = {0.f, 0.f, 0.f, 0.f};          // of no weight, whatever the values hold
-      if (l != 0.f) {
-        x = o[i][dt] * f;
-        if (odd) {
+      if (l != 0.f) x = o[i][dt] * f;
+      if (odd && (l != 0.f || a.splits > 1)) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (last[i] >= s_up[d + e]) x[e] += INFINITY;
-            if (last[i] >= s_down[d + e]) x[e] -= INFINITY;
-          }
+        for (int e = 0; e < 4; ++e) {
+          const bool up = last[i] >= s_up[d + e], down = last[i] >= s_down[d + e];
+          // NaN of both, and of a sum that is NaN
+          if (up || down) x[e] = (up ? INFINITY : 0.f) + (down ? -INFINITY : 0.f) + (l - l);
         }
       }
       if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part_o + to * a.D + d) = x;

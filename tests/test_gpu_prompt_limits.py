@@ -187,3 +187,61 @@ def test_references_behind_the_maximum(R, dtype):
     for j in range(6, R):
         x[j] += (j % 17) * (at >= V - 1 - 37 * j)
     _check_logprobs(x, g.integers(0, V, (R, 2)), 4, dtype)
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,n,m", [
+    ("bf16", 4, 2, 64, 150, 150), ("bf16", 8, 2, 128, 300, 300), ("bf16", 6, 2, 40, 700, 700),
+    ("bf16", 4, 2, 128, 30, 3000), ("bf16", 4, 2, 256, 90, 900), ("bf16", 8, 2, 128, 200, 4300),
+    ("bf16", 8, 2, 64, 4500, 4500), ("f32", 4, 2, 64, 150, 150), ("f32", 4, 2, 128, 200, 1500),
+    ("f32", 4, 2, 64, 600, 600)])
+def test_infinite_values_of_a_prompt_whatever_their_weight(dtype, Hq, Hkv, D, n, m):
+    """A query that sees an infinite value gets it, NaN of a NaN or of both signs, be the
+    key's weight 0, below float32 or large, wherever in its keys the key stands."""
+    g = np.random.default_rng(n + D)
+    q, k, v = (to_dev(draw(g, dtype, r, h, D)) for r, h in ((n, Hq), (m, Hkv), (m, Hkv)))
+    q[:, :, 0], k[:, :, 0] = 1.0, 0.0
+    own = m - n // 2                                 # some query's own key, and one before all
+    for at in (own, 5):
+        k[at, :, 0] = -INF                           # weight 0
+        k[at + 1, :, 0] = -3e4                       # weight e^-3750 and less
+        k[at + 2, :, 0] = 40.0
+    clean, lse = ops.prompt_attention(q, k, v)
+    assert torch.isfinite(clean).all()
+    for at in (own, 5):
+        w = v.clone()
+        w[at, 0, 3], w[at + 1, 0, 4], w[at + 2, 0, 5] = INF, -INF, INF
+        w[at, 1, D - 1], w[at + 1, 1, D - 1] = -INF, INF
+        w[at, 1, 2] = NAN
+        out, l = ops.prompt_attention(q, k, w)
+        assert torch.equal(l, lse)
+        token = torch.arange(n)[:, None].expand(n, Hkv) + (m - n)
+        want = clean.clone()
+        for h, d, key, x in ((0, 3, at, INF), (0, 4, at + 1, -INF), (0, 5, at + 2, INF),
+                             (1, D - 1, at, -INF), (1, 2, at, NAN), (1, D - 1, at + 1, NAN)):
+            _set(want, token[:, h] >= key, h, Hq // Hkv, d, x)
+        same = (out == want) | (torch.isnan(out) & torch.isnan(want))
+        assert same.all(), (at, (~same).nonzero()[:5])
+
+
+def _set(want, rows, h, per, d, x):
+    part = want[:, h * per:(h + 1) * per, d]
+    part[rows.to(DEV)] = x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_values_behind_keys_of_no_weight(dtype):
+    # all keys of a first part of the history, which blocks of their own take
+    n, m, D = 3, 5000, 64
+    g = np.random.default_rng(m)
+    q, k, v = (to_dev(draw(g, dtype, r, h, D)) for r, h in ((n, 4), (m, 2), (m, 2)))
+    q[:, :, 0], k[:, :, 0], k[:2000, :, 0] = 1.0, 0.0, -INF
+    clean, lse = ops.prompt_attention(q, k, v)
+    v[20, 0, 1], v[1900, 1, 7], v[1950, 1, 7] = -INF, INF, INF
+    v[4990, 0, 9] = NAN
+    out, l = ops.prompt_attention(q, k, v)
+    clean[:, :2, 1], clean[:, 2:, 7], clean[:, :2, 9] = -INF, INF, NAN
+    same = (out == clean) | (torch.isnan(out) & torch.isnan(clean))
+    assert same.all() and torch.equal(l, lse)
+    k[2000:, :, 0] = -INF                            # no weight at all
+    out, l = ops.prompt_attention(q, k, v)
+    assert (out == 0).all() and (l == -INF).all()
