@@ -150,9 +150,9 @@ int moe_kv4_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, int32
  * places hold -1 and -inf. A row of nothing but -inf: logprobs -inf, entropy 0. A row
  * with a NaN or +inf: logprobs (of tokens in 0..V-1) and entropy NaN, top_tokens -1,
  * top_logprobs -inf.
- * Numerics: float32 exponentials of differences to a reference within 8 of the maximum
- * of what it stands for, summed in float64 beyond 32 of them, the best logit's terms
- * apart where they are most of the sum. A log-probability is off by at most 2^-15 of the
+ * Numerics: float32 exponentials of differences to a reference that no logit exceeds by
+ * more than 8, summed in float64 beyond 32 of them, the best logit's terms apart where
+ * they are most of the sum. A log-probability is off by at most 2^-15 of the
  * best token's own, the entropy by at most 2^-13 of itself, beside the rounding to
  * float32: no log-probability is above 0, no entropy below, and both are 0 where one
  * token has all.
@@ -162,11 +162,10 @@ int moe_kv4_attention(const void* q, int32_t dtype, int64_t R, int32_t Hq, int32
  * tokens  [R, m] int32 (NULL when m == 0); logprobs [R, m] float32
  * entropy [R] float32 or NULL
  * top_tokens [R, n_top] int32, top_logprobs [R, n_top] float32 (NULL when n_top == 0)
- * workspace  moe_token_logprobs_workspace bytes, 256-byte aligned (may be 0); a size
- *         that does not fall as R, V or n_top grows: that of the largest call serves all
+ * workspace  none is needed: the size is 0, and what is given is not used
  * Limits: R, V >= 1, m >= 0, 0 <= n_top <= 64, V <= 2^24, R < 2^22, R * m < 2^31,
  *   stride < 2^31; one output at least (m, entropy or n_top).
- * Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP.
+ * Errors: MOE_ERR_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_HIP.
  * ---------------------------------------------------------------------- */
 size_t moe_token_logprobs_workspace(int64_t R, int64_t V, int64_t m, int32_t n_top);
 int moe_token_logprobs(const void* logits, int32_t dtype, int64_t R, int64_t V, int64_t stride,
