@@ -738,29 +738,40 @@ def load_experts(store, cache, expert_ids, slot_ids, stream=None):
 _CURRENT = contextlib.nullcontext()
 
 
-def _one_device(stream, *ts):
-    """Every given tensor contiguous, on one GPU: a context in which that is the
-    current device and `stream`, if there is one, the current stream, so that what
-    the call allocates or fills belongs to the stream that it goes to."""
-    dev = None                         # a tensor of the host is -1
-    for t in ts:
-        if t is None:
-            continue
-        d = t.get_device()
-        if d != dev:
-            if d < 0:
-                raise ValueError("every tensor must be on the GPU")
-            if dev is not None:
-                raise ValueError("every tensor must be on the same GPU")
-            dev = d
-        if not t.is_contiguous():
-            raise ValueError("every tensor must be contiguous")
+def _first_device(dev, d):
+    """The device of a call's tensors: that of the first, d, where no tensor was before
+    it (dev None; a tensor of the host is -1). Called where d is not dev."""
+    if d < 0:
+        raise ValueError("every tensor must be on the GPU")
+    if dev is not None:
+        raise ValueError("every tensor must be on the same GPU")
+    return d
+
+
+def _on(dev, stream):
+    """A context in which dev is the current device and `stream`, if there is one, the
+    current stream, so that what the call allocates or fills belongs to the stream that
+    it goes to."""
     cuda = _torch().cuda
     if stream is not None:
         if stream.device.index != dev:
             raise ValueError("the stream must be of the tensors' GPU")
         return cuda.stream(stream)
     return _CURRENT if dev == cuda.current_device() else cuda.device(dev)
+
+
+def _one_device(stream, *ts):
+    """Every given tensor contiguous, on one GPU: a context as of _on."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        d = t.get_device()
+        if d != dev:
+            dev = _first_device(dev, d)
+        if not t.is_contiguous():
+            raise ValueError("every tensor must be contiguous")
+    return _on(dev, stream)
 
 
 def _want(name, t, shape, dtype):
@@ -1008,15 +1019,11 @@ def _checked(stream, strided, *specs):
     """_one_device and _want in one pass, for calls whose time is the host's. specs:
     (name, tensor or None, shape or None, dtype or None), contiguous; strided: tensors
     whose layout has been checked."""
-    dev = None                         # a tensor of the host is -1
+    dev = None
     for t in strided:
         d = t.get_device()
         if d != dev:
-            if d < 0:
-                raise ValueError("every tensor must be on the GPU")
-            if dev is not None:
-                raise ValueError("every tensor must be on the same GPU")
-            dev = d
+            dev = _first_device(dev, d)
     for name, t, shape, dtype in specs:
         if t is None:
             continue
@@ -1024,19 +1031,10 @@ def _checked(stream, strided, *specs):
             raise ValueError(f"{name} must be {dtype} {'' if shape is None else list(shape)}")
         d = t.get_device()
         if d != dev:
-            if d < 0:
-                raise ValueError("every tensor must be on the GPU")
-            if dev is not None:
-                raise ValueError("every tensor must be on the same GPU")
-            dev = d
+            dev = _first_device(dev, d)
         if not t.is_contiguous():
             raise ValueError("every tensor must be contiguous")
-    cuda = _torch().cuda
-    if stream is not None:
-        if stream.device.index != dev:
-            raise ValueError("the stream must be of the tensors' GPU")
-        return cuda.stream(stream)
-    return _CURRENT if dev == cuda.current_device() else cuda.device(dev)
+    return _on(dev, stream)
 
 
 def prompt_attention_workspace(N, M, B, Hq, Hkv, D, dtype_code=MOE_BF16):
