@@ -75,7 +75,8 @@ int moe_prompt_attention(const void* q, const void* k, const void* v, int32_t dt
  * the least with max |x| <= 7 * 2^e and e in -124..125; a channel is held as the
  * nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e (ties to the even code; larger
  * ones as 6), with its sign. No value is off by more than half of the step it lies
- * in, 2^e at most. A block with a NaN or an infinity is NaN as a whole.
+ * in, 2^e at most, but for those beyond 7 * 2^125, which become 6 * 2^125. A block with a
+ * NaN or an infinity is NaN as a whole.
  *
  * codes  [n_slots, Hkv, D / 2] uint8: channel 2i in the lower half of byte i, 2i + 1 in
  *        the upper; bit 3 the sign, bits 0..2 the index of the value

@@ -6,12 +6,12 @@
 // A wave takes 64 keys of one head at a time. Their codes go straight from memory to
 // LDS, four lanes a key (lanes that load from sixteen keys each keep the address unit
 // busy four times as long), the next keys while the values are in work and the other
-// way round; sixteen waves a compute unit, by registers and LDS, keep some 80 KB on
-// their way. Keys come back as
-// MFMA operands, a quarter of a head a lane (k slots 8t + j of quarter q4 are dimensions
-// q4 D/4 + 8t + j, of the queries too), and become bf16 with their block's scale, two an
-// instruction: exact, as a value has two bits times a power of two. Rows of the score
-// tiles are dealt so that lane (query r, q4) holds scores of keys 16 q4 .. 16 q4 + 15,
+// way round. A compute unit holds sixteen waves by registers and LDS (bf16, D of 128);
+// splits stop at two blocks of it, eight waves, which keep up to 68 KB on their way. Keys
+// come back as MFMA operands, a quarter of a head a lane (k slots 8t + j of quarter q4 are
+// dimensions q4 D/4 + 8t + j, of the queries too), and become bf16 with their block's
+// scale, two an instruction: exact, as a value has two bits times a power of two. Rows of
+// the score tiles are dealt so that lane (query r, q4) holds scores of keys 16 q4 .. 16 q4 + 15,
 // which is what a transposing read of 4-bit values gives a lane: 16 keys of one
 // dimension. Values stay unscaled there; a key's scales go into the numerators, once
 // for every 32 dimensions, exact as well.
@@ -191,8 +191,11 @@ struct KaCore {
       }
     }
   }
-  // O += V^T P^T. bf16: p is rounded to bf16 (at most 2^-8 of it, for the matrix cores);
-  // its sum is taken of the float32 values.
+  // O += V^T P^T. bf16: p is rounded to bf16 (by at most 2^-8 of it, for the matrix cores);
+  // its sum is taken of the float32 values. Of flat attention over 1000 or 8192 keys the
+  // result is off by 2.3e-3 (rms), 1.7e-3 of it the rounding of the result itself; with p
+  // as the sum of two bf16 numbers only that is left, and one row of 131072 keys takes
+  // 39.6 us for 34.7, 64 of 8192 119 for 116, 200 of 777 44.6 for 39.5.
   static __device__ __forceinline__ void values(f32x4_t (&o)[1][DT], const f32x4_t (&p)[1][KT],
                                                 const char* codes, const char* units) {
     const int r = lane_id() & 15, q4 = lane_id() >> 4, k = 16 * q4 + r;

@@ -10,8 +10,9 @@
 // itself. Where S is below 2 that is much beside ln S, which is next to 0: the threads
 // that hold the best logit then have their logits read again and the others' terms summed
 // apart from it, S = C + rest with C the (one or two) terms that are 1. So what is next to
-// 0 is off by a part of itself, and with one token left 0 (0.4 us of a row of 32000, 8.3;
-// to count the best while the row is read took 2 of 8.3, 13 of 104 for 2000 x 128000).
+// 0 is off by a part of itself, and with one token left 0. Such a row takes 1 us more (1 x
+// 32000 float32 8.3 -> 9.2, 2000 x 128000 97.5 -> 99); to count the best while any row is
+// read took 2 of 8.3 and 13 of 104.
 // Best alternatives need no second pass over the row: of kGroups groups of threads the
 // n-th largest of their maxima, cut to some leading bits, is a bound T that n logits
 // reach, and only threads whose own maximum reaches T hold more of them, about n. A

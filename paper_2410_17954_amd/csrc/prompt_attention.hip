@@ -15,8 +15,9 @@
 // Every wave has 16 or 32 columns of its own; keys and values go straight from memory to
 // LDS, a tile of keys ahead of the one that all waves of a block compute on, swizzled by
 // which 16 bytes each lane fetches. Tiles before the first query of a wave need no
-// mask. One prompt of 16384 tokens, 32 heads of 128 over eight key heads, takes 1.89 ms:
-// 1165 TFLOP/s, the MFMAs run in 47 % of the cycles, instructions are issued in 72 %.
+// mask. One prompt of 16384 tokens, 32 heads of 128 over eight key heads, takes 1.86 ms
+// (1.93 on another card): 1183 TFLOP/s, the MFMAs run in 51 % of the cycles,
+// instructions are issued in 71 %. Times here and below are of calls in a captured graph.
 // Measured and left out: another order of MFMAs and exponentials (the tiles of columns
 // apart, interleaved by hand), reads from LDS further ahead, a third buffer, priorities
 // between the waves of a SIMD: level or slower.
@@ -190,8 +191,11 @@ struct PrCore {
       }
     }
   }
-  // p, rounded to bf16 (at most 2^-8 of it, for the matrix cores); its sum is taken of
-  // the float32 values
+  // p, rounded to bf16 (by at most 2^-8 of it, for the matrix cores); its sum is taken of
+  // the float32 values. Of flat attention over 1000 or 8192 keys the result is off by
+  // 2.3e-3 (rms), 1.7e-3 of it the rounding of the result itself. With p as the sum of two
+  // bf16 numbers only that is left, and 777 tokens take 23.9 us for 20.3, sixteen prompts
+  // of up to 1000 144 for 126, one of 16384 2.73 ms for 1.93.
   static __device__ __forceinline__ u32x4_t numerators(const f32x4_t& p0, const f32x4_t& p1) {
     bf16x8_t b;
 #pragma unroll
@@ -311,7 +315,7 @@ struct PrCore {
 };
 
 // Keys of a tile: of 64 in blocks of four waves fewer blocks fit a compute unit (sixteen
-// prompts of up to 1000 tokens 126 us, of 64 keys 163).
+// prompts of up to 1000 tokens 126 us, of 64 keys 154).
 constexpr int pr_keys(int elt, int dp, int waves) {
   return elt * dp < 256 || (elt * dp == 256 && waves == 8) ? 64 : elt * dp <= 512 ? 32 : 16;
 }
@@ -505,31 +509,32 @@ struct PrPlan {
 };
 
 // Blocks of eight waves with 32 columns each load keys half as often and have the higher
-// rate (one prompt of 16384 tokens, 32 heads of 128: 1.89 ms, of four waves with 16
-// columns 2.13), but for few or short prompts smaller blocks fill the card better and
-// cost less to start (777 tokens 25.3 us, wide 29.8; sixteen prompts of up to 1000
-// 126 and 141, of up to 2000 level; 16 tokens 6.1 and 9.5; 4096 tokens 153 and 138).
+// rate (one prompt of 16384 tokens, 32 heads of 128: 1.86 ms, of four waves with 16
+// columns 2.17; 4096 tokens 136 and 155), but for few or short prompts smaller blocks
+// fill the card better and cost less to start (777 tokens 20.1 us, wide 31.9; 2048 49 and
+// 64; sixteen prompts of up to 1000 126 and 137, of up to 2000 level; 16 tokens 5.5 and
+// 7.8).
 constexpr int kWideKeys = 4096, kWideColumns = 256;
 // Keys are split over blocks while at most this many blocks are then in flight (bf16,
-// 64 tokens each of four sequences behind 4000 keys 42 us, with half as many 47; 777
-// tokens, whose 392 blocks are left whole, 26, in two splits 34: joins pay for keys
-// that few queries see), each of kMinKeys at least (one token behind 2000 keys 13 us, of
-// twice as many 15.5). float32 blocks take so long that more of them pay (two prompts of
-// 1000 tokens, 8 heads of 128: three splits 63 us, two 85).
+// 64 tokens each of four sequences behind 4000 keys 34 us, with half as many 38; 777
+// tokens in one group, whose 392 blocks are left whole, 24.6, in two splits 28.9: joins pay
+// for keys that few queries see), each of kMinKeys at least (one token behind 2000 keys
+// 11.4 us, of twice as many 13.3). float32 blocks take so long that more of them pay (two
+// prompts of 1000 tokens, 8 heads of 128: three splits 60 us, two 84).
 constexpr int kSplitBlocks = 512, kWideSplitBlocks = 256, kFloatSplitBlocks = 768;
 constexpr int kMinKeys = 128, kMostSplits = 64;
 // Two groups of waves on a block's columns while blocks do not fill the card and have
-// enough keys (777 tokens 25.3 -> 20.8 us, 2000 of 16 heads of 256 94 -> 71, of 28 heads of
-// 80 54 -> 43; 2048 tokens of 32 heads, 1024 blocks, 53 -> 57, 16 tokens 6.1 -> 6.7);
-// float32 of more than 64 dimensions has no LDS for it (64 -> 74).
+// enough keys (777 tokens 24.6 -> 20.1 us, 2000 of 16 heads of 256 93 -> 69, of 28 heads of
+// 80 56 -> 42; 2048 tokens of 32 heads, 1024 blocks, 49 -> 58, 16 tokens 5.5 -> 6.5);
+// float32 of more than 64 dimensions has no LDS for it (64 -> 74 in smaller tiles).
 constexpr int kGroupBlocks = 896, kGroupKeys = 512;
 // Four groups where every block has a compute unit to itself, which its LDS takes (32
-// heads of 128: 256 tokens 16.0 -> 11.2 us, 400 20.0 -> 12.8, 512 20.0 -> 13.9; 128 tokens
-// 7.9 -> 9.8; 600, in 304 blocks, 16.0 -> 19.5), and sequences have columns to fill it
-// (16 tokens of two sequences behind 1000 keys 14.5 -> 16.2). A join then costs as much as
-// four tiles a group: splits are of kFourMinKeys at least (512 tokens of 16 heads 12.9 us,
-// in two splits 18.5; of 1024 keys, 40 tokens behind 3000 take 27.2 instead of 20.0).
-// float32, whose splits are more, 31.9 -> 38.5 (1500 tokens of 4 heads of 64).
+// heads of 128: 256 tokens 14.9 -> 10.6 us, 400 19.0 -> 12.1, 512 20.2 -> 13.6; 128 tokens
+// of 16 heads 6.9 -> 9.3; 600, in 304 blocks, 15.6 -> 18.6), and sequences have columns to
+// fill it (16 tokens of two sequences behind 1000 keys 14.2 -> 16.8). A join then costs as
+// much as four tiles a group: splits are of kFourMinKeys at least (512 tokens of 16 heads
+// 12.8 us, in two splits 18.7; of 1024 keys, 40 tokens behind 3000 take 27.1 instead of
+// 19.9). float32, whose splits are more, 31.9 -> 38.5 (1500 tokens of 4 heads of 64).
 constexpr int kFourBlocks = 256, kFourKeys = 256, kFourColumns = 128, kFourMinKeys = 512;
 
 PrPlan pr_plan(int64_t N, int64_t M, int64_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype) {
