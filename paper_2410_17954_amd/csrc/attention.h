@@ -98,8 +98,8 @@ inline ScoreScale score_scale(float scale, bool bf16) {
 }
 
 // ---------------------------------------------------------------- join
-// part_o [splits][RH][D], part_ml [splits][RH] (maximum in log2, sum; sum 0: o is not
-// read) -> out [RH, D], lse [RH] of the rows offsets[0] .. offsets[n_off - 1] - 1 (RH /
+// part_o [splits][RH][D], part_ml [splits][RH] (reference in log2, sum; sum 0: o is not
+// read; of a reference of -inf any other sum adds 0, o only what is no number) -> out [RH, D], lse [RH] of the rows offsets[0] .. offsets[n_off - 1] - 1 (RH /
 // heads rows; all without offsets).
 struct JoinArgs {
   const float* part_o;

@@ -401,7 +401,8 @@ ka_kernel(KaArgs a) {
   }
   if (r >= cols) return;
   if (q4 == 0) {
-    if (a.splits > 1) a.part_ml[to] = make_float2(top, l);
+    // keys without weight may have values of NaN: their sum, of a maximum of -inf, adds 0
+    if (a.splits > 1) a.part_ml[to] = make_float2(top, l == 0.f ? 1.f : l);
     else if (a.lse) a.lse[at] = lse_of(top, l);
   }
   const float inv = 1.f / l;                     // of no weight: 0, whatever the values hold

@@ -245,3 +245,29 @@ def test_infinite_values_behind_keys_of_no_weight(dtype):
     k[2000:, :, 0] = -INF                            # no weight at all
     out, l = ops.prompt_attention(q, k, v)
     assert (out == 0).all() and (l == -INF).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hkv,R", [(1, 1), (4, 2), (2, 300)])
+def test_nan_values_of_a_cache_of_4_bits_whatever_their_weight(Hkv, R, dtype):
+    """Keys of weight 0 (scores of -inf), single ones and all of a first part, which
+    blocks of their own take where rows are few: their blocks of NaN count."""
+    g = np.random.default_rng(R)
+    S, D = 1500, 64
+    k, v = (to_dev(draw(g, "f32", S, Hkv, D)) for _ in range(2))
+    k[:, :, 0] = 0.0
+    k[:600, :, 0], k[1000, :, 0] = 2.0, 2.0
+    cache, _ = _kv4(k, v)
+    q = to_dev(draw(g, dtype, R, 2 * Hkv, D))
+    q[:, :, 0] = -3e38                               # times 2 and more: -inf
+    rows = torch.zeros(R, dtype=torch.int32, device=DEV)
+    clean, lse = ops.kv4_attention(q, cache, cache_row=rows, scale=0.2)
+    assert torch.isfinite(clean).all() and torch.isfinite(lse).all()
+    for key, h, block in ((20, 0, 0), (599, Hkv - 1, 1), (1000, 0, 1), (1400, Hkv - 1, 0)):
+        held = cache[3].clone()
+        held[0, key, h, block] = 255
+        out, l = ops.kv4_attention(q, cache[:3] + (held,), cache_row=rows, scale=0.2)
+        want = clean.clone()
+        want[:, 2 * h:2 * h + 2, 32 * block:32 * block + 32] = NAN
+        same = (out == want) | (torch.isnan(out) & torch.isnan(want))
+        assert same.all() and torch.equal(l, lse), (key, (~same).nonzero()[:4])
