@@ -118,7 +118,7 @@ int moe_kv4_load(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t*
  * and accumulation; with float32 q products are of 24 bits, with bf16 the softmax
  * numerators are rounded to bf16 for the second product, their sum is not. Large values
  * as for moe_prompt_attention (one key of 6 * 2^125 is held); terms below 2^-100 may lose
- * bits, below 2^-115 count as 0. Results do not depend on scheduling. lse joins the
+ * bits, below 2^-115 may count as 0. Results do not depend on scheduling. lse joins the
  * result with that over other keys (moe_prefix_attention).
  *
  * q, out     [R, Hq, D] dtype; lse [R, Hq] float32 or NULL

@@ -271,3 +271,29 @@ def test_nan_values_of_a_cache_of_4_bits_whatever_their_weight(Hkv, R, dtype):
         want[:, 2 * h:2 * h + 2, 32 * block:32 * block + 32] = NAN
         same = (out == want) | (torch.isnan(out) & torch.isnan(want))
         assert same.all() and torch.equal(l, lse), (key, (~same).nonzero()[:4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_small_values(dtype):
+    """Values of some 2^-75 in a cache and 2^-95 in a prompt are as exact as others: terms
+    of 2^-20 of them are above what may lose bits (2^-100, 2^-118)."""
+    g = np.random.default_rng(8)
+    S, D, n = 300, 64, 40
+    k, v = draw(g, "f32", S, 1, D, std=0.3), draw(g, "f32", S, 1, D)
+    q = to_dev(draw(g, dtype, n, 2, D))
+    # a cache: values of some 2^-75
+    cache, (kk, vv) = _kv4(to_dev(k), to_dev(v * 2.0 ** -75))
+    lens = torch.arange(S - n + 1, S + 1, dtype=torch.int32, device=DEV)
+    rows = torch.zeros(n, dtype=torch.int32, device=DEV)
+    out, lse = ops.kv4_attention(q, cache, lens=lens, cache_row=rows, scale=0.125)
+    # a prompt: of some 2^-95
+    t = _dtype(dtype)
+    pk, pv = to_dev(k).to(t), to_dev(v * 2.0 ** -95).to(t)
+    pout, plse = ops.prompt_attention(q, pk, pv, scale=0.125)
+    for got, l, k64, v64, up in ((out, lse, kk, vv, 2.0 ** 75), (pout, plse, vals(pk), vals(pv), 2.0 ** 95)):
+        for r in (0, n // 2, n - 1):
+            for h in range(2):
+                m, x = S - n + r + 1, vals(q)[r, h]
+                ref, rl = oracle.prompt.softmax_rows(0.125 * (k64[:m, 0] @ x), v64[:m, 0] * up)
+                check_row(vals(got)[r, h] * up, to_host(l)[r, h], ref, rl, x, k64[:m, 0],
+                          v64[:m, 0] * up, 0.125, dtype)
