@@ -44,7 +44,7 @@ def test_infinite_queries_over_a_cache_of_4_bits(D, S, dtype):
     assert (out[0, 0] == 0).all() and lse[0, 0] == -INF
     # infinity less infinity, and a NaN: no numbers
     assert torch.isnan(out[0, 1:3]).all() and torch.isnan(lse[0, 1:3]).all()
-    x = vals(q)[0, 3]
+    x = vals(q[0, 3])
     ref, rl = oracle.prompt.softmax_rows(0.1 * (kk[:, 0] @ x), vv[:, 0])
     check_row(vals(out)[0, 3], to_host(lse)[0, 3], ref, rl, x, kk[:, 0], vv[:, 0], 0.1, dtype)
     cache[3][:, ::5] = 255                           # whatever the values hold
